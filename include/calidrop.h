@@ -22,6 +22,10 @@
  * caller workspace).  The field calib_size of the parameters is the calibration size of
  * Section 4.4.
  *
+ * Beside them, for the prefill that precedes a compression and for requests that are not compressed:
+ * calidrop_paged_append, calidrop_paged_prefill, calidrop_paged_decode and
+ * calidrop_paged_prefix_decode over a cache in pages.
+ *
  * Conventions
  *   - Unless a comment says HOST, every tensor pointer is a DEVICE pointer to a contiguous,
  *     16-byte aligned buffer on the current device.  "bf16" buffers hold bfloat16 values.
@@ -443,6 +447,133 @@ int calidrop_decode_host(const calidrop_params* p,
                          const float* O_c, const float* LSE_c, const void* C_q,
                          void* out, float* lse_out, uint8_t* flags,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A KV cache in pages, and the attention over it.
+ *
+ * calidrop_compress takes the keys and values of a whole prompt, and its row LSE, from a prefill; a
+ * batch in service also holds requests that are not (or not yet) compressed.  These entry points are
+ * that side of it: queries and keys are rotated and appended (calidrop_paged_append), the new tokens
+ * attend to the cache (calidrop_paged_prefill; one token a sequence: calidrop_paged_decode; sequences
+ * that share a long prefix: calidrop_paged_prefix_decode).  The paper has no counterpart; the window
+ * with sinks is its StreamingLLM baseline (Sections 4.1.2 and 4.1.3), taken as a mask on the whole
+ * cache instead of a kept list, and the shared prefix is joined with Eq. 1.
+ *
+ *   Layout.  K_pages, V_pages: [n_pages][Hkv][page_size][D]; page_stride elements lie between two
+ *   pages (0: Hkv * page_size * D), so that K and V may be the halves of one pool.  Row t of sequence
+ *   b is row t % page_size of page block_table[b * max_pages + t / page_size].  Pages may lie anywhere
+ *   and be shared by sequences (that are not appended to).  Queries, keys and values of the new tokens
+ *   are packed, sequence after sequence: [n_tokens][heads][D], q_stride / k_stride / v_stride elements
+ *   between two tokens (0: heads * D), so that they may be parts of a fused projection's output.
+ *   Sequence b has the tokens q_start[b] .. q_start[b+1]-1; tokens at and beyond q_start[B] are padding:
+ *   they are not read and their outputs stay as they are.
+ *   Lengths and tables are DEVICE arrays, read on the stream: a captured graph may be replayed after
+ *   they have changed.  kv_len[b] counts the rows of sequence b INCLUDING its new tokens, for the
+ *   append as well as for the attention: new token i of n sits at position kv_len[b] - n + i.
+ *
+ *   Bad device data (a page index outside [0, n_pages) for a row that is needed, a length outside
+ *   [0, max_pages * page_size], a q_start that falls or passes n_tokens, a position outside the table of
+ *   angles) is caught by the kernels: nothing is read or written out of bounds, the sequence's results
+ *   are undefined and the workspace's first 32-bit word becomes non-zero (bit 0: lengths, bit 1: page,
+ *   bit 2: position; other bits: a wait inside a kernel ran out).  The word stays until the caller clears it.
+ *
+ *   Values in rows [0, kv_len) are expected to be finite in calidrop_paged_prefill: an infinite or NaN
+ *   value may also reach tokens of the same sequence that do not see it.  Elsewhere, and for K
+ *   everywhere, what is masked or lies in rows and pages that are not visible has no effect,
+ *   whatever it holds.
+ */
+#define CALIDROP_BF16 0
+#define CALIDROP_FP16 1
+#define CALIDROP_MAX_SEQUENCES 4096
+
+typedef struct calidrop_paged_params {
+  int32_t B, Hq, Hkv, D;        /* sequences; D must be 128; Hq % Hkv == 0; G = Hq/Hkv <= 8        */
+  int32_t dtype;                /* CALIDROP_BF16 or CALIDROP_FP16: queries, cache and outputs        */
+  int32_t page_size;            /* 16, 32, 64, 128 or 256 rows                                       */
+  int32_t n_pages;              /* pages of the pool                                                 */
+  int32_t max_pages;            /* entries of a sequence's row of the block table                    */
+  int32_t window;               /* attention: a query at position p sees the keys t <= p with        */
+  int32_t n_sink;               /* t > p - window or t < n_sink; window 0: all t <= p                */
+  int32_t rot_dim;              /* append: leading elements of a head that are rotated, a multiple   */
+                                /* of 16 up to D; 0: none                                            */
+  int32_t interleaved;          /* 0: element i turns with i + rot_dim/2; 1: 2i with 2i + 1          */
+  int32_t max_pos;              /* rows of the table of angles                                       */
+  int32_t n_groups;             /* prefix_decode: groups of sequences that share a prefix            */
+  int32_t max_prefix_pages;     /* prefix_decode: entries of a row of the prefix table               */
+  float   softmax_scale;        /* 0 => 1/sqrt(D)                                                    */
+  int64_t q_stride, k_stride, v_stride;   /* elements between two tokens, multiples of 8; 0: packed  */
+  int64_t page_stride;          /* elements between two pages, a multiple of 8; 0: packed            */
+} calidrop_paged_params;
+
+/*
+ * Bytes of scratch that every calidrop_paged_* call needs for these parameters and up to n_tokens new
+ * tokens (0 if they are invalid).  256-byte aligned; zeroed once before its first use
+ * (calidrop_decode_workspace_init); every call leaves it ready for the next.  Calls that overlap on
+ * the device must not share a workspace; calls of different kinds may use the same one in turn.
+ */
+size_t calidrop_paged_workspace_bytes(const calidrop_paged_params* p, int32_t n_tokens);
+
+/*
+ * Rotate the new tokens' queries and keys by their positions and store keys and values into the cache.
+ * With c = cos_sin[pos][i] and s = cos_sin[pos][rot_dim/2 + i], the pair (x1, x2) of index i becomes
+ * (x1 c - x2 s, x2 c + x1 s), in 32 bits and rounded once; the remaining elements and V are copied.
+ *
+ *   q        in  [n_tokens][Hq][D] or NULL (then q_out is not written)
+ *   k, v     in  [n_tokens][Hkv][D]
+ *   positions in [n_tokens] i32 or NULL: the position that a token is rotated by, where that is not
+ *            its place in the cache
+ *   cos_sin  in  [max_pos][rot_dim] f32: cosines, then sines; NULL with rot_dim = 0
+ *   K_pages, V_pages in/out; block_table [B][max_pages] i32, q_start [B+1] i32, kv_len [B] i32 in
+ *   q_out    out [n_tokens][Hq][D], packed; may be q where that is packed
+ * Two tokens with the same place in the cache race.  A token with bad data (see above) is left out as a
+ * whole.  n_tokens = 0 does nothing.
+ * Errors: INVALID_ARG (null or misaligned pointers, sizes, strides), UNSUPPORTED (D, G, page_size,
+ * rot_dim, dtype, B > CALIDROP_MAX_SEQUENCES, not sm_100), WORKSPACE_TOO_SMALL, CUDA_ERROR.
+ */
+int calidrop_paged_append(const calidrop_paged_params* p, int32_t n_tokens, const void* q, const void* k, const void* v,
+                          const int32_t* positions, const float* cos_sin, void* K_pages, void* V_pages,
+                          const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* q_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of the new tokens of a ragged batch over the cache, which holds their keys and values already:
+ * causal, with the window and the sinks of `p`.  Sequences may have any number of new tokens (none, one,
+ * a chunk, a whole prompt) on top of any number of cached rows.
+ *
+ *   q        in  [n_tokens][Hq][D] as the attention sees them
+ *   out      out [n_tokens][Hq][D], packed
+ *   lse      out [n_tokens][Hq] f32 or NULL: natural logarithm of the softmax denominator
+ * A token that sees no key (its position is negative: kv_len[b] is less than the number of new tokens)
+ * gets out = 0, lse = -inf.  The last window rows of `lse`, transposed, are the lse_obs of calidrop_compress.
+ * Errors as above.
+ */
+int calidrop_paged_prefill(const calidrop_paged_params* p, int32_t n_tokens, const void* q, const void* K_pages,
+                           const void* V_pages, const int32_t* block_table, const int32_t* q_start,
+                           const int32_t* kv_len, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * The same for one new token a sequence (token b belongs to sequence b, n_tokens = B): its position is
+ * kv_len[b] - 1.  A sequence without rows gets out = 0, lse = -inf.
+ */
+int calidrop_paged_decode(const calidrop_paged_params* p, const void* q, const void* K_pages, const void* V_pages,
+                          const int32_t* block_table, const int32_t* kv_len, void* out, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * One new token a sequence, where the sequences group_start[g] .. group_start[g+1]-1 share the rows
+ * [0, prefix_len[g]) that the row g of prefix_table names, ahead of the kv_len[b] rows of their own
+ * (0 is allowed).  The rows of a prefix are read once for the whole group, on the tensor cores, and
+ * joined with each sequence's own rows by Eq. 1; sequences outside all groups have their own rows only.
+ *
+ *   group_start [n_groups+1] i32, prefix_table [n_groups][max_prefix_pages] i32, prefix_len [n_groups] i32 in
+ *   the rest as for calidrop_paged_decode
+ * window must be 0 (UNSUPPORTED).
+ */
+int calidrop_paged_prefix_decode(const calidrop_paged_params* p, const void* q, const void* K_pages, const void* V_pages,
+                                 const int32_t* group_start, const int32_t* prefix_table, const int32_t* prefix_len,
+                                 const int32_t* block_table, const int32_t* kv_len, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable text for a status code; for CALIDROP_CUDA_ERROR includes the last CUDA
  * error string seen by the calling thread. */

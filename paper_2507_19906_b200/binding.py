@@ -39,6 +39,8 @@ EXPORTS = [
     "calidrop_decode_workspace_bytes", "calidrop_decode_workspace_init",
     "calidrop_decode_workspace_status_offset", "calidrop_decode_plan", "calidrop_decode",
     "calidrop_decode_batched", "calidrop_decode_static", "calidrop_compress_host", "calidrop_decode_host",
+    "calidrop_paged_workspace_bytes", "calidrop_paged_append", "calidrop_paged_prefill", "calidrop_paged_decode",
+    "calidrop_paged_prefix_decode",
     "calidrop_status_string", "calidrop_version", "calidrop_launch_count",
 ]
 
@@ -48,6 +50,14 @@ class Params(C.Structure):
                 ("B", "Hq", "Hkv", "D", "L", "window", "pool", "budget", "n_cal", "cap")] + \
                [("softmax_scale", C.c_float), ("theta1", C.c_float), ("theta2", C.c_float),
                 ("calib_size", C.c_int32)]
+
+
+class PagedParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in
+                ("B", "Hq", "Hkv", "D", "dtype", "page_size", "n_pages", "max_pages", "window", "n_sink", "rot_dim",
+                 "interleaved", "max_pos", "n_groups", "max_prefix_pages")] + \
+               [("softmax_scale", C.c_float)] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "page_stride")]
 
 
 class CompressLayout(C.Structure):
@@ -75,7 +85,7 @@ def _load_native():
     loader = importlib.machinery.ExtensionFileLoader("_marshal", MARSHAL_PATH)
     module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_marshal", loader))
     loader.exec_module(module)
-    module.open(LIB_PATH, Params, DecodeLayer)
+    module.open(LIB_PATH, Params, DecodeLayer, PagedParams)
     return module
 
 
@@ -133,6 +143,14 @@ def load():
     lib.calidrop_compress_host.argtypes = [C.POINTER(Params)] + [vp] * 18 + [C.c_size_t, vp]
     lib.calidrop_decode_host.restype = C.c_int
     lib.calidrop_decode_host.argtypes = [C.POINTER(Params)] + [vp] * 11 + [C.c_int32] + [vp] * 7 + [C.c_size_t, vp]
+    lib.calidrop_paged_workspace_bytes.restype = C.c_size_t
+    lib.calidrop_paged_workspace_bytes.argtypes = [C.POINTER(PagedParams), C.c_int32]
+    for f, n in ((lib.calidrop_paged_append, 11), (lib.calidrop_paged_prefill, 8)):
+        f.restype = C.c_int
+        f.argtypes = [C.POINTER(PagedParams), C.c_int32] + [vp] * (n + 1) + [C.c_size_t, vp]
+    for f, n in ((lib.calidrop_paged_decode, 7), (lib.calidrop_paged_prefix_decode, 10)):
+        f.restype = C.c_int
+        f.argtypes = [C.POINTER(PagedParams)] + [vp] * (n + 1) + [C.c_size_t, vp]
     lib.calidrop_status_string.restype = C.c_char_p
     lib.calidrop_status_string.argtypes = [C.c_int]
     lib.calidrop_version.restype = C.c_int
@@ -315,6 +333,57 @@ def calidrop_decode_static(p, q, k_new, v_new, K_kept, V_kept, kv_len, O_c, LSE_
     rc = (_native or native()).decode_static(p, q, k_new, v_new, K_kept, V_kept, kv_len, O_c, LSE_c, C_q, out, lse_out, flags)
     if check:
         _check(rc, "calidrop_decode_static")
+    return rc
+
+
+PAGED_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def make_paged_params(*, B, Hq, Hkv, page_size, n_pages, max_pages, dtype=torch.bfloat16, D=128, window=0, n_sink=0,
+                      rot_dim=0, interleaved=False, max_pos=0, n_groups=0, max_prefix_pages=0, softmax_scale=0.0,
+                      q_stride=0, k_stride=0, v_stride=0, page_stride=0) -> PagedParams:
+    return PagedParams(B=B, Hq=Hq, Hkv=Hkv, D=D, dtype=PAGED_DTYPES.get(dtype, dtype), page_size=page_size,
+                       n_pages=n_pages, max_pages=max_pages, window=window, n_sink=n_sink, rot_dim=rot_dim,
+                       interleaved=int(interleaved), max_pos=max_pos, n_groups=n_groups,
+                       max_prefix_pages=max_prefix_pages, softmax_scale=softmax_scale, q_stride=q_stride,
+                       k_stride=k_stride, v_stride=v_stride, page_stride=page_stride)
+
+
+def calidrop_paged_workspace_bytes(p: PagedParams, n_tokens: int) -> int:
+    return int(load().calidrop_paged_workspace_bytes(C.byref(p), n_tokens))
+
+
+def calidrop_paged_append(p, q, k, v, positions, cos_sin, K_pages, V_pages, block_table, q_start, kv_len, q_out,
+                          workspace, check=True) -> int:
+    """q, k and v may be views with the token strides of `p` (k.shape[0] tokens), the pages views with its page stride."""
+    rc = (_native or native()).paged_append(p, q, k, v, positions, cos_sin, K_pages, V_pages, block_table, q_start, kv_len,
+                                            q_out, workspace)
+    if check and rc:
+        _check(rc, "calidrop_paged_append")
+    return rc
+
+
+def calidrop_paged_prefill(p, q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, check=True) -> int:
+    """q.shape[0] tokens."""
+    rc = (_native or native()).paged_prefill(p, q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace)
+    if check and rc:
+        _check(rc, "calidrop_paged_prefill")
+    return rc
+
+
+def calidrop_paged_decode(p, q, K_pages, V_pages, block_table, kv_len, out, lse, workspace, check=True) -> int:
+    rc = (_native or native()).paged_decode(p, q, K_pages, V_pages, block_table, kv_len, out, lse, workspace)
+    if check and rc:
+        _check(rc, "calidrop_paged_decode")
+    return rc
+
+
+def calidrop_paged_prefix_decode(p, q, K_pages, V_pages, group_start, prefix_table, prefix_len, block_table, kv_len, out,
+                                 lse, workspace, check=True) -> int:
+    rc = (_native or native()).paged_prefix_decode(p, q, K_pages, V_pages, group_start, prefix_table, prefix_len, block_table,
+                                                   kv_len, out, lse, workspace)
+    if check and rc:
+        _check(rc, "calidrop_paged_prefix_decode")
     return rc
 
 

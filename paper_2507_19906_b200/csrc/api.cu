@@ -21,11 +21,6 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int cuda_fail(cudaError_t e) {
-  snprintf(g_err_text, sizeof g_err_text, "CUDA error: %s", cudaGetErrorString(e));
-  return CALIDROP_CUDA_ERROR;
-}
-
 // Parameter checks shared by every entry point that reads the full struct.
 int check_common(const calidrop_params* p) {
   if (!p) return CALIDROP_INVALID_ARG;
@@ -99,19 +94,6 @@ CompressWs make_ws(const CompressGeom& g) {
   }
   w.total = off;
   return w;
-}
-
-int device_supported() {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  static int major_of[64];
-  if (dev < 0 || dev >= 64) return 0;
-  if (major_of[dev] == 0) {
-    int major = 0;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return 0;
-    major_of[dev] = major;
-  }
-  return major_of[dev] == 10;
 }
 
 // The most CTAs that may share a unit: a launch whose units are split has one CTA per SM at most (a CTA's ring then
@@ -225,6 +207,24 @@ int static_scratch_ptr(void** out) {
 }
 
 }  // namespace
+
+int cuda_fail(cudaError_t e) {
+  snprintf(g_err_text, sizeof g_err_text, "CUDA error: %s", cudaGetErrorString(e));
+  return CALIDROP_CUDA_ERROR;
+}
+
+int device_supported() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  static int major_of[64];
+  if (dev < 0 || dev >= 64) return 0;
+  if (major_of[dev] == 0) {
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return 0;
+    major_of[dev] = major;
+  }
+  return major_of[dev] == 10;
+}
 
 void count_launch(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 

@@ -189,6 +189,9 @@ cudaError_t launch_calib_none(const CompressGeom& g, const void* Q_obs, float* O
                               cudaStream_t st);
 
 void count_launch(int n = 1);
+// api.cu: the status code for a CUDA error, whose text is kept for the calling thread; whether the current device is sm_100
+int cuda_fail(cudaError_t e);
+int device_supported();
 
 #ifdef __CUDACC__
 // Lets `kernel` use `bytes` of dynamic shared memory, once per device; `done` is the kernel's own.  Threads may race

@@ -7,6 +7,7 @@
 // host's pace.  Measured per calidrop_decode call, host time: 11.2 -> 3.1 us; a
 // token of eight layers, called layer by layer: 89 -> 59 us at 4 kv heads x 4333 rows, 89 -> 72 us at 32 x 2111.
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -17,13 +18,15 @@ namespace {
 
 #define CALIDROP_ENTRIES(X)                                                                                         \
   X(compress) X(calibrate) X(gather_evicted) X(recalibrate) X(accumulated_scores) X(select_from_scores)             \
-  X(select_streaming) X(decode) X(decode_batched) X(decode_static)
+  X(select_streaming) X(decode) X(decode_batched) X(decode_static)                                                  \
+  X(paged_append) X(paged_prefill) X(paged_decode) X(paged_prefix_decode)
 #define DECLARE(name) decltype(&calidrop_##name) f_##name = nullptr;
 CALIDROP_ENTRIES(DECLARE)
 #undef DECLARE
 
 PyTypeObject* params_type = nullptr;   // the binding's ctypes structures (see open)
 PyTypeObject* layer_type = nullptr;
+PyTypeObject* paged_type = nullptr;
 
 // The positional arguments of one call.  A conversion that fails sets a Python error, after which `ok` is
 // false and the entry point is not called.
@@ -137,6 +140,64 @@ struct Args {
     ok = false;
     return nullptr;
   }
+  const calidrop_paged_params* paged(int i) {
+    if (!ok) return nullptr;
+    if (PyObject_TypeCheck(a[i], paged_type)) return (const calidrop_paged_params*)buf(i);
+    PyErr_SetString(PyExc_TypeError, "a PagedParams structure expected");
+    ok = false;
+    return nullptr;
+  }
+  // Device pointer of a tensor whose first dimension may have a stride of its own: `stride` elements (0: what its packed
+  // form has), the others packed.  An address or None is taken as it is.
+  void* rows(int i, int64_t stride) {
+    PyObject* o = a[i];
+    if (!ok || o == Py_None || !THPVariable_CheckExact(o)) return ptr(i);
+    try {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      int64_t want = 1;
+      bool same = t.dim() > 0;
+      for (int64_t d = t.dim() - 1; same && d >= 1; --d) {
+        same = t.size(d) == 1 || t.stride(d) == want;
+        want *= t.size(d);
+      }
+      same = same && (t.size(0) <= 1 || t.stride(0) == (stride ? stride : want));
+      if (same) return t.data_ptr();
+      PyErr_SetString(PyExc_AssertionError, "the tensor's strides are not those of the parameters");
+      ok = false;
+      return nullptr;
+    } catch (...) {
+    }
+    return ptr(i);
+  }
+  // No tensor of another device, and none of the host's: its address would mean nothing to the kernels.
+  void on_this_device(Py_ssize_t n) {
+    for (Py_ssize_t i = 1; ok && i < n; ++i) {
+      if (!THPVariable_CheckExact(a[i])) continue;
+      try {
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (t.is_cuda() && t.get_device() == c10::cuda::current_device()) continue;
+        PyErr_SetString(PyExc_ValueError, "tensors on the current CUDA device expected");
+      } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+      }
+      ok = false;
+    }
+  }
+  // the first dimension of a tensor
+  int32_t tokens(int i) {
+    PyObject* s = ok ? PyObject_GetAttrString(a[i], "shape") : nullptr;
+    PyObject* n = s ? PySequence_GetItem(s, 0) : nullptr;
+    Py_XDECREF(s);
+    const long v = n ? PyLong_AsLong(n) : -1;
+    Py_XDECREF(n);
+    if (!n || (v == -1 && PyErr_Occurred())) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "a tensor expected");
+      ok = false;
+      return 0;
+    }
+    if (v != (int32_t)v) { PyErr_SetString(PyExc_OverflowError, "more tokens than int32 counts"); ok = false; }
+    return (int32_t)v;
+  }
   const calidrop_decode_layer* layers(int i) {
     if (!ok) return nullptr;
     PyObject* element = PyObject_GetAttrString((PyObject*)Py_TYPE(a[i]), "_type_");   // of an array type
@@ -198,21 +259,42 @@ ENTRY(decode_batched, 4, x.params(0), (int32_t)x.len(1), x.layers(1), x.i32(2), 
 ENTRY(decode_static, 13, x.params(0), x.ptr(1), x.ptr(2), x.ptr(3), x.ptr(4), x.ptr(5), x.i32(6), (const float*)x.ptr(7),
       (const float*)x.ptr(8), x.ptr(9), x.ptr(10), (float*)x.ptr(11), (uint8_t*)x.ptr(12))
 
-// open(path, Params, DecodeLayer): the shared library whose entry points the functions forward to, and the ctypes
+#define PAGED_ENTRY(name, n_args, ...)                                                  \
+  PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {                 \
+    Args x(args, n, n_args);                                                            \
+    const calidrop_paged_params* p = x.paged(0);                                        \
+    x.on_this_device(n);                                                                \
+    if (!x.ok) return nullptr;                                                          \
+    return forward(x, f_##name, p, __VA_ARGS__);                                        \
+  }
+PAGED_ENTRY(paged_append, 13, x.tokens(2), x.rows(1, p->q_stride), x.rows(2, p->k_stride), x.rows(3, p->v_stride),
+            (const int32_t*)x.ptr(4), (const float*)x.ptr(5), x.rows(6, p->page_stride), x.rows(7, p->page_stride),
+            (const int32_t*)x.ptr(8), (const int32_t*)x.ptr(9), (const int32_t*)x.ptr(10), x.ptr(11), x.ptr(12), x.nbytes(12))
+PAGED_ENTRY(paged_prefill, 10, x.tokens(1), x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+            (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), (const int32_t*)x.ptr(6), x.ptr(7), (float*)x.ptr(8), x.ptr(9),
+            x.nbytes(9))
+PAGED_ENTRY(paged_decode, 9, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+            (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), x.ptr(6), (float*)x.ptr(7), x.ptr(8), x.nbytes(8))
+PAGED_ENTRY(paged_prefix_decode, 12, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+            (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), (const int32_t*)x.ptr(6), (const int32_t*)x.ptr(7),
+            (const int32_t*)x.ptr(8), x.ptr(9), (float*)x.ptr(10), x.ptr(11), x.nbytes(11))
+
+// open(path, Params, DecodeLayer, PagedParams): the shared library whose entry points the functions forward to, and the ctypes
 // structures of its arguments
 PyObject* py_open(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 3 || !PyType_Check(args[1]) || !PyType_Check(args[2]))
-    return PyErr_Format(PyExc_TypeError, "a path and two structure types expected");
+  if (n != 4 || !PyType_Check(args[1]) || !PyType_Check(args[2]) || !PyType_Check(args[3]))
+    return PyErr_Format(PyExc_TypeError, "a path and three structure types expected");
+  const size_t sizes[4] = {0, sizeof(calidrop_params), sizeof(calidrop_decode_layer), sizeof(calidrop_paged_params)};
   const char* s = PyUnicode_AsUTF8(args[0]);
   if (!s) return nullptr;
-  for (int i = 1; i < 3; ++i) {
+  for (int i = 1; i < 4; ++i) {
     PyObject* o = PyObject_CallNoArgs(args[i]);
     Py_buffer v;
     if (!o) return nullptr;
     const bool buffer = PyObject_GetBuffer(o, &v, PyBUF_SIMPLE) == 0;
     Py_DECREF(o);
     if (!buffer) return nullptr;
-    const bool same = v.len == (Py_ssize_t)(i == 1 ? sizeof(calidrop_params) : sizeof(calidrop_decode_layer));
+    const bool same = v.len == (Py_ssize_t)sizes[i];
     PyBuffer_Release(&v);
     if (!same) return PyErr_Format(PyExc_TypeError, "the structure's size is not the library's");
   }
@@ -225,6 +307,7 @@ PyObject* py_open(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #undef RESOLVE
   params_type = (PyTypeObject*)Py_NewRef(args[1]);
   layer_type = (PyTypeObject*)Py_NewRef(args[2]);
+  paged_type = (PyTypeObject*)Py_NewRef(args[3]);
   Py_RETURN_NONE;
 }
 

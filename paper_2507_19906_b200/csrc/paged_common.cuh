@@ -1,0 +1,106 @@
+// Device helpers of the kernels over a cache in pages: 16-bit types, TMA copies of page boxes.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "paged.h"
+#include "tc_common.cuh"
+
+namespace calidrop {
+
+// P is rounded to the type of V for the product P V.  In fp16 the probabilities are kept 2^kBias higher than their sum's
+// reference says, so that small ones keep their bits (a probability of 2^-14 of the largest would be subnormal); in bf16 there is
+// nothing to gain.
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  if constexpr (kF16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    return pack_bf16(a, b);
+  }
+}
+template <bool kF16>
+__device__ __forceinline__ float2 unpack16(uint32_t x) {
+  if constexpr (kF16) return __half22float2(*reinterpret_cast<__half2*>(&x));
+  else return make_float2(bf16_lo(x), bf16_hi(x));
+}
+
+// D(16x8, f32) += A(16x16, row) * B(16x8, col) in either type
+template <bool kF16>
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+  if constexpr (kF16) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  } else {
+    mma_bf16_16816(c, a0, a1, a2, a3, b0, b1);
+  }
+}
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3,
+                                            int c4, uint64_t pol) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "l"(pol)
+      : "memory");
+}
+
+// Rows [0, kv) of a sequence that a query at its last position sees, in blocks of 2^kLg rows: near_blocks from the first on,
+// then those from `first` on.
+struct PagedView {
+  int kv, lo;            // rows at and beyond lo are inside the window
+  int near_blocks, first, n_blocks;
+  __device__ __forceinline__ int block(int j) const { return j < near_blocks ? j : j - near_blocks + first; }
+};
+template <int kLg>
+__device__ __forceinline__ PagedView paged_view(int kv, int window, int n_sink) {
+  PagedView v;
+  v.kv = kv;
+  v.lo = window && kv > window ? kv - window : 0;
+  const int blocks = (kv + (1 << kLg) - 1) >> kLg;
+  v.first = v.lo >> kLg;
+  // (in 64 bits: n_sink may be anything)
+  const int sink_blocks = (int)min((long long)v.first, ((long long)n_sink + (1 << kLg) - 1) >> kLg);
+  v.near_blocks = sink_blocks;
+  v.n_blocks = max(1, sink_blocks + blocks - v.first);   // (a sequence without rows has one block, of which nothing is visible)
+  return v;
+}
+
+// Four outputs of a partial softmax, its maximum (or whatever its terms are relative to) and its sum, all in the log2 domain.
+struct Partial {
+  float o[4], m, l;
+  __device__ __forceinline__ void join(float m2, float l2, const float4& o2) {
+    const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+    const float f1 = ex2_approx(m - ref), f2 = ex2_approx(m2 - ref);
+    l = l * f1 + l2 * f2;
+    o[0] = o[0] * f1 + o2.x * f2; o[1] = o[1] * f1 + o2.y * f2;
+    o[2] = o[2] * f1 + o2.z * f2; o[3] = o[3] * f1 + o2.w * f2;
+    m = mn;
+  }
+};
+
+// Rows `row(i)` of n partial rows of kStride floats, this lane's four outputs of each, joined in order.
+template <typename Row>
+__device__ __forceinline__ void join_rows(Partial& p, int n, int lane, Row row) {
+  constexpr int kBatch = 4;   // loads in flight
+  for (int i0 = 0; i0 < n; i0 += kBatch) {
+    float4 o[kBatch];
+    float2 ml[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const float* r = row(min(i0 + i, n - 1));
+      o[i] = __ldcg(reinterpret_cast<const float4*>(r) + lane);
+      ml[i] = __ldcg(reinterpret_cast<const float2*>(r + kD));
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (i0 + i < n) p.join(ml[i].x, ml[i].y, o[i]);
+  }
+}
+
+}  // namespace calidrop
