@@ -9,11 +9,13 @@
 // cache), and the list is in falling order of cost, dealt to the persistent CTAs forwards and backwards in turn.  What was cut is
 // joined by paged_combine_kernel, or by the decode kernel.
 //
-// A CTA works on two streams of 128 rows, one warpgroup each, a thread to a row; while one stream has its softmax the other
-// has the tensor cores.  Tensor memory: S of the streams at columns 0 and 128, O at 256 and 384.  P, rounded to 16 bits,
-// overwrites the first 64 columns of its S.  One warp issues all MMAs, and those of an issuing thread run in order, so
+// A CTA works on two streams of 128 rows; while one stream has its softmax the other has the tensor cores.  A stream is two
+// warpgroups, two threads to a row, 64 of a tile's keys each.  Tensor memory: S of the streams at columns 0 and 128, O at 256 and
+// 384.  P, rounded to 16 bits, overwrites S, the first 32 of the 64 columns of each warpgroup.  One warp issues all MMAs, and those of
+// an issuing thread run in order, so
 //   * S(j+1) may be issued behind P V(j), which reads P from the same columns;
 //   * a stream that has been told of S(j) also knows that its P V(j-1) is done, and may rescale O itself.
+// P is handed over in two halves, so that P V begins while the second is worked on.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over its reference, which on real logits is a few times a
 // row; until then terms are at most 2^8, and the sums and O hold that in 32 bits.
 #include <algorithm>
@@ -29,12 +31,20 @@ namespace {
 
 using namespace tc;
 
-constexpr int kSoftmaxWarps = 8;                  // two streams of four
-constexpr int kProducerWarp = 8, kMmaWarp = 9, kQWarp = 10;
-constexpr int kThreads = 384;
+constexpr int kSoftmaxWarps = 16;                 // two streams of two warpgroups
+constexpr int kProducerWarp = 16, kMmaWarp = 17, kQWarp = 18;
+constexpr int kThreads = 640;
 constexpr int kSlots = 5;                         // K and V tiles in one ring, in the order in which they are used
 constexpr int kTileBytes = kKvTileBytes;          // 32 KB
-constexpr int kSmemBytes = (2 + kSlots) * kTileBytes + 1024;
+// What is in shared memory beside the two query blocks and the ring.
+struct Tail {
+  unsigned long long bars[2 * kSlots + 12];
+  float max[2][2][128];                           // [stream][half][row]: maxima of a tile's halves, and at the end the sums
+  uint32_t tmem;
+  Ctl ctl;
+};
+constexpr int kSmemBytes = (2 + kSlots) * kTileBytes + sizeof(Tail);
+static_assert(kSmemBytes <= 227 * 1024, "all of it: there is no static shared memory, so that the tiles begin at a multiple of 1024");
 constexpr uint32_t kColO = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kBuckets = 256;
@@ -259,23 +269,20 @@ template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                        const __grid_constant__ CUtensorMap v_map, const KernelArgs a) {
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long bars[2 * kSlots + 10];
-  __shared__ uint32_t tmem_slot;
-  __shared__ Ctl ctl;
+  extern __shared__ __align__(1024) unsigned char smem_al[];
+  Tail& tail = *reinterpret_cast<Tail*>(smem_al + (2 + kSlots) * kTileBytes);
+  Ctl& ctl = tail.ctl;
 
   const PagedGeom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_base = smem_base, ring = smem_base + 2 * kTileBytes;
-  unsigned char* const smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t bar0 = smem_u32(bars);
+  const uint32_t q_base = smem_u32(smem_al), ring = q_base + 2 * kTileBytes;
+  const uint32_t bar0 = smem_u32(tail.bars);
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (kSlots + s); };
   auto q_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (2 * kSlots + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 4 + s); };
-  auto p_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 6 + s); };
+  auto p_full = [&](int s, int part) { return bar0 + 8u * (2 * kSlots + 6 + (part ? 4 : 0) + s); };
   auto o_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 8 + s); };
 
   if (tid == 0) {
@@ -284,12 +291,12 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     for (int s = 0; s < kSlots; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1);
-      mbar_init(s_full(s), 1); mbar_init(p_full(s), 128); mbar_init(o_full(s), 1);
+      mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 256); mbar_init(p_full(s, 1), 256); mbar_init(o_full(s), 1);
     }
     fence_mbar_init();
   }
   if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(&tmem_slot), 512);
+    tmem_alloc(smem_u32(&tail.tmem), 512);
     tmem_relinquish();
   }
   // rows of the query blocks that no copy writes (128 is not a multiple of G) hold zeros
@@ -298,7 +305,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem_base = tmem_slot;
+  const uint32_t tmem_base = tail.tmem;
   pdl_wait();
   const int n_work = a.head->n_items * g.Hkv;
   const int R = a.tokens;
@@ -399,14 +406,19 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       }
       __syncwarp();
     };
-    auto issue_pv = [&](int s, int v_slot, bool first) {
+    // P V of the keys of part 0 (0..31 and 64..95 of the tile) or 1; the P of keys 64.. sits at columns 64..
+    auto issue_pv = [&](int s, int v_slot, int part, bool first) {
       if (leader) {
         const uint32_t d = tmem_base + kColO + (uint32_t)(s * 128), p = tmem_base + (uint32_t)(s * 128);
         const uint64_t vd = desc_advance(dv, (uint32_t)v_slot * kTileBytes);
-        umma_ts(d, p, vd, idesc_o, first ? 0u : 1u);
 #pragma unroll
-        for (int kk = 1; kk < kTileKeys / 16; ++kk)
-          umma_ts_imm<1>(d, p + (uint32_t)(kk * 8), desc_advance(vd, (uint32_t)kk * 16u * kLineBytes), idesc_o);
+        for (int i = 0; i < 4; ++i) {
+          const int kk = (i >> 1) * 4 + (i & 1);           // the step of part 0; that of part 1 is two on
+          const uint32_t col = p + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8) + (part ? 16u : 0u);
+          const uint64_t v = desc_advance(vd, ((uint32_t)kk + (part ? 2u : 0u)) * 16u * kLineBytes);
+          if (i == 0) umma_ts(d, col, v, idesc_o, first ? 0u : 1u);
+          else umma_ts_imm<1>(d, col, v, idesc_o);
+        }
       }
       __syncwarp();
     };
@@ -451,11 +463,15 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const bool more = j + 1 < n;
         for (int s = 0; s < 2; ++s) {
           if (s == 1 && !dual) break;
-          ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, p_full(s), pph[s], 0x500u));
+          ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, p_full(s, 0), pph[s], 0x500u));
+          if (!ok) break;
+          tc_fence_after_sync();
+          issue_pv(s, vs, 0, j == 0);
+          ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, p_full(s, 1), pph[s], 0x580u));
           pph[s] ^= 1u;
           if (!ok) break;
           tc_fence_after_sync();
-          issue_pv(s, vs, j == 0);
+          issue_pv(s, vs, 1, false);
           if (!more) {
             commit(o_full(s));
           } else {
@@ -472,15 +488,19 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       }
     }
   } else if (warp < kSoftmaxWarps) {
-    // ------------------------------------------------------------ softmax: a thread to a row
+    // ------------------------------------------------------------ softmax: two threads to a row
     constexpr float kBias = kF16 ? 7.f : 0.f;     // (see pack16; with the 2^8 of the lazy rescaling below the largest fp16)
     constexpr float kLazy = 8.f;
-    const int s = warp >> 2, r = tid & 127;
+    const int s = warp >> 3, half = (warp >> 2) & 1, r = tid & 127;
     const uint32_t lane_bits = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem_base + lane_bits + (uint32_t)(s * 128), o_addr = s_addr + kColO;
+    const uint32_t s_addr = tmem_base + lane_bits + (uint32_t)(s * 128 + half * 64), o_addr = s_addr + kColO;
     const int i_tok = s * R + r / g.G, head = r - (r / g.G) * g.G;
     const bool in_block = r < R * g.G;
     const f32x2 sc = pack2(g.scale2);
+    // (read by the other warpgroup before it hands over its P: whoever sees the next S may write again)
+    volatile float* const my_max = &tail.max[s][half][r];
+    const volatile float* const other_max = &tail.max[s][half ^ 1][r];
+    auto meet = [&]() { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + s) : "memory"); };   // the stream's two warpgroups
     uint32_t sph = 0, oph = 0;
     bool ok = true;
     Deal deal(n_work);
@@ -493,59 +513,64 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       // the keys from clear_lo (or from the first, as far as the sinks go) up to clear_hi are seen by all rows of the stream
       const int clear_hi = min(it.kv_end, it.pos0 + s * R + 1);
       const int clear_lo = g.window ? it.pos0 + tok_last - g.window + 1 : 0;
-      float ref = -INFINITY, l = 0.f;       // reference of the row's terms (log2 domain), their sum
+      float ref = -INFINITY, l = 0.f;       // reference of the row's terms (log2 domain), the sum of this thread's
 #pragma unroll 1
       for (int j = 0; j < it.n_steps; ++j) {
         const int row0 = (it.step0 + j < it.near_tiles ? it.step0 + j : it.step0 + j + it.skip) * kTileKeys;
+        // (a wait that runs out leaves the loop together with the other warps of the stream, or they would wait at `meet`: both
+        // see the same barrier, and none of the phases behind it will complete)
         ok = __all_sync(0xffffffffu, mbar_wait(&ctl, s_full(s), sph, 0x600u));
-        if (!ok) break;
         sph ^= 1u;
         tc_fence_after_sync();
-        uint32_t x[4][32];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld32_issue(s_addr + 32 * q, x[q]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld_wait(x[q]);
+        uint32_t x[2][32];
+        tmem_ld32_issue(s_addr, x[0]);
+        tmem_ld32_issue(s_addr + 32, x[1]);
+        tmem_ld_wait(x[0]);
+        tmem_ld_wait(x[1]);
         if (row0 + kTileKeys > clear_hi || (row0 < clear_lo && row0 + kTileKeys > g.n_sink)) {
-          const int hi = min(it.kv_end, pos + 1) - row0;                 // keys below it
-          const int lo = g.window ? pos - g.window + 1 - row0 : 0;       // keys from it on, and the sinks
-          const int sink = g.n_sink - row0;
+          const int key0 = row0 + half * 64;
+          auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // the n lowest bits
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < 2; ++q) {
+            const int k0 = key0 + 32 * q;
+            uint32_t seen = below(min(it.kv_end, pos + 1) - k0);
+            if (g.window) seen &= ~below(pos - g.window + 1 - k0) | below(g.n_sink - k0);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const int t = 32 * q + c;
-              if (!(t < hi && (t >= lo || t < sink))) x[q][c] = 0xff800000u;
-            }
+            for (int c = 0; c < 32; ++c)
+              if (!((seen >> c) & 1u)) x[q][c] = 0xff800000u;
+          }
         }
         float mx[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          mx[q] = __uint_as_float(x[q][0]);
+          mx[q] = __uint_as_float(x[q >> 1][(q & 1) * 16]);
 #pragma unroll
-          for (int c = 1; c < 32; ++c) mx[q] = fmaxf(mx[q], __uint_as_float(x[q][c]));
+          for (int c = 1; c < 16; ++c) mx[q] = fmaxf(mx[q], __uint_as_float(x[q >> 1][(q & 1) * 16 + c]));
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * g.scale2 - kBias;
+        float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        *my_max = top;
+        meet();
+        top = fmaxf(top, *other_max) * g.scale2 - kBias;
         const bool grow = top > ref + kLazy;             // (from -inf on the first key that is seen)
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? ex2_approx(ref - top) : 1.f;
           const bool had = __any_sync(0xffffffffu, grow && ref > -INFINITY);
           if (grow) { l *= f; ref = top; }
-          if (had && j > 0) {
+          if (had && j > 0) {                            // this half of O's columns
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
-              uint32_t o[32];
-              tmem_ld32(o_addr + 32 * q, o);
+              uint32_t o[16];
+              tmem_ld16(o_addr + 16 * q, o);
 #pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-              tmem_st32(o_addr + 32 * q, o);
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+              tmem_st16(o_addr + 16 * q, o);
             }
           }
         }
         const f32x2 nref = pack2(ref == -INFINITY ? 0.f : -ref);
         f32x2 sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 2; ++q) {
           uint32_t packed[16];
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
@@ -556,26 +581,33 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             packed[c >> 1] = pack16<kF16>(p.x, p.y);
           }
           tmem_st16(s_addr + 16 * q, packed);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          mbar_arrive(p_full(s, q));
         }
         const float2 t = unpack2(add2(sum0, sum1));
         l += t.x + t.y;
-        tmem_st_wait();
-        tc_fence_before_sync();
-        mbar_arrive(p_full(s));
+        if (!ok) break;
       }
       if (!ok) break;
       ok = __all_sync(0xffffffffu, mbar_wait(&ctl, o_full(s), oph, 0x700u));
-      if (!ok) break;
       oph ^= 1u;
       tc_fence_after_sync();
+      // the row's sum, of the lower keys and the upper ones in this order
+      *my_max = l;
+      meet();
+      const float l_other = *other_max;
+      l = half ? l_other + l : l + l_other;
+      meet();                                            // (the next item writes there)
+      if (!ok) break;
       const bool valid = in_block && i_tok < it.n_tok;
       if (it.part_row < 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;        // no key seen: zeros
         const size_t row = (size_t)(it.tok0 + i_tok) * g.Hq + h * g.G + head;
-        uint4* const dst = reinterpret_cast<uint4*>(a.out) + row * (kD / 8);
+        uint4* const dst = reinterpret_cast<uint4*>(a.out) + row * (kD / 8) + half * 8;
         const bool store = valid && it.part_row == -1;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 2; ++q) {
           uint32_t o[32];
           tmem_ld32(o_addr + 32 * q, o);
           if (store) {
@@ -590,20 +622,20 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             }
           }
         }
-        if (store && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
+        if (store && a.lse && half == 0) a.lse[row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
       } else {
         float* const dst = a.parts + ((size_t)it.part_row + (size_t)h * it.rows + (size_t)i_tok * g.G + head) * kPagedPartStride;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 2; ++q) {
           uint32_t o[32];
           tmem_ld32(o_addr + 32 * q, o);
           if (valid) {
 #pragma unroll
             for (int c = 0; c < 32; c += 4)
-              *reinterpret_cast<uint4*>(dst + 32 * q + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+              *reinterpret_cast<uint4*>(dst + half * 64 + 32 * q + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
           }
         }
-        if (valid) *reinterpret_cast<float2*>(dst + kD) = make_float2(ref, l);
+        if (valid && half == 0) *reinterpret_cast<float2*>(dst + kD) = make_float2(ref, l);
       }
     }
   }
