@@ -1,5 +1,4 @@
-// What the kernels over a cache in pages share: the geometry of a call, the layout of its workspace, the work list of the
-// tensor-core attention, and the launchers.
+// What the kernels over a cache in pages share: the geometry of a call, the layout of its workspace, and the launchers.
 #pragma once
 
 #include "internal.h"
@@ -32,33 +31,14 @@ constexpr size_t kPagedPlan = kPagedDecodeParts + (size_t)kPagedMaxCtas * 2 * kM
 static_assert(kPagedMaxCtas * 4 <= 4096 && kPagedPlan % 256 == 0, "");
 
 struct PagedWs {
-  size_t items, tiles, part_o, total;
-  int max_tiles, max_items, max_split;
+  size_t sched, heavy, tokens, part_o, total;
   long long max_rows;          // partial rows
 };
 
-// One item of the tensor-core attention's work list, for each kv head: up to 256 query rows (token-major, the group's heads within)
-// against a range of steps, each a tile of 128 keys.
-struct PagedItem {
-  int tok0, n_tok;       // its tokens
-  int seq;               // whose row of the block table
-  int pos0;              // position of the first token
-  int kv_end;            // keys at and beyond it are seen by none of the tokens
-  int win_lo;            // keys in [n_sink, win_lo) neither
-  int near_tiles, skip;  // step j is tile j, or j + skip from step near_tiles on
-  int step0, n_steps;
-  int part_row;          // first partial row of head 0, or -1: the results are final
-  int rows;              // partial rows of a head
-};
-static_assert(sizeof(PagedItem) == 48, "read as three 16-byte vectors");
-
-// What became of a tile of query rows: its chunks' partial rows lie at part_row + (chunk * Hkv + head) * rows.
-struct PagedTile {
-  int part_row, n_chunks, rows, tok0;
-};
-
-struct PagedPlanHeader {
-  int n_items, n_tiles, n_split, pad;
+// Where the attention of a sequence's query token over a shared prefix lies: chunk c of head g of kv head h is partial row
+// part_row + c * chunk_rows + h * head_rows + g.
+struct PagedToken {
+  int part_row, n_chunks, chunk_rows, head_rows;
 };
 
 // paged_append.cu

@@ -62,6 +62,32 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 
+// 64 fp32 columns of 16 lanes of tensor memory, a lane's columns spread over four threads: thread t has of lane t / 4 (and t / 4 + 8)
+// columns 8 c + 2 (t % 4) and the next one in r[4 c], r[4 c + 1] (and r[4 c + 2], r[4 c + 3]), c = 0..7.
+__device__ __forceinline__ void tmem_ld_16x64(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+
+// Thread q of a quad gives v[c] to thread c and has the values of threads 0..3 for itself.
+__device__ __forceinline__ uint4 quad_transpose(const uint32_t (&v)[4], int lane) {
+  const bool odd = lane & 1, up = lane & 2;
+  const uint32_t x0 = __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 1), x1 = __shfl_xor_sync(0xffffffffu, odd ? v[2] : v[3], 1);
+  const uint32_t a0 = odd ? x0 : v[0], a1 = odd ? v[1] : x0;     // value (q & 1) of threads q & 2 and the next
+  const uint32_t b0 = odd ? x1 : v[2], b1 = odd ? v[3] : x1;     // value (q & 1) + 2
+  const uint32_t y0 = __shfl_xor_sync(0xffffffffu, up ? a0 : b0, 2), y1 = __shfl_xor_sync(0xffffffffu, up ? a1 : b1, 2);
+  return up ? make_uint4(y0, y1, b0, b1) : make_uint4(a0, a1, y0, y1);
+}
+
 // Rows [0, kv) of a sequence that a query at its last position sees, in blocks of 2^kLg rows: near_blocks from the first on,
 // then those from `first` on.
 struct PagedView {
@@ -86,6 +112,7 @@ __device__ __forceinline__ PagedView paged_view(int kv, int window, int n_sink) 
 // Four outputs of a partial softmax, its maximum (or whatever its terms are relative to) and its sum, all in the log2 domain.
 struct Partial {
   float o[4], m, l;
+  __device__ __forceinline__ void clear() { o[0] = o[1] = o[2] = o[3] = 0.f; m = -INFINITY; l = 0.f; }
   __device__ __forceinline__ void join(float m2, float l2, const float4& o2) {
     const float mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
     const float f1 = ex2_approx(m - ref), f2 = ex2_approx(m2 - ref);

@@ -10,9 +10,11 @@
 // that is cut each CTA leaves its partial (outputs, maximum, sum), and the last of them to arrive joins these, in the order of
 // the parts, so that the result does not depend on who is last.
 //
-// A CTA is a producer warp and eight stream warps, as in decode.cu: K and V come through a ring of six slots of 64 rows by
-// TMA, a copy per page and slot, and a slot is consumed by four warps of 16 rows with mma.sync, keys on the 16-row side.  The
-// producer runs ahead over the borders of units, so that the memory does not wait for a unit's end.
+// A CTA is a producer warp and four stream warps: K and V come through a ring of three slots of 64 rows by TMA, a copy per page and
+// slot, and a slot is consumed by the four warps, 16 rows each, with mma.sync, keys on the 16-row side (as in decode.cu).  The
+// producer runs ahead over the borders of units, so that the memory does not wait for a unit's end, and two CTAs share an SM, so that
+// one streams while the other ends a unit.  (One CTA of eight stream warps and six slots: 768 units of 24 to 600 rows, joined with
+// a shared prefix, 87 us.)
 #include <algorithm>
 
 #include "paged_common.cuh"
@@ -23,13 +25,24 @@ bool paged_kv_map(CUtensorMap* out, const void* base, const PagedGeom& g, int ro
 
 namespace {
 
-constexpr int kSlots = 6, kSlotRows = 64, kLgRows = 6;
-constexpr int kStreamWarps = 8, kThreads = (kStreamWarps + 1) * 32;
+constexpr int kSlots = 3, kSlotRows = 64, kLgRows = 6;
+constexpr int kStreamWarps = 4, kThreads = (kStreamWarps + 1) * 32;
+constexpr int kCtas = 2 * kSms;                        // two to an SM
 constexpr int kPartBytes = kSlotRows * kRowBytes;      // K or V of a slot: 16 KB
 constexpr int kSlotBytes = 2 * kPartBytes;
 constexpr int kStride = kPagedPartStride;              // floats of a warp's partial row: heads land in distinct banks
-constexpr int kSmemBytes = kSlots * kSlotBytes + kStreamWarps * kMaxG * kStride * 4 + 1024;
-constexpr int kMinBlocks = 1;                          // blocks of a CTA at least
+constexpr int kUnitCost = 1;                           // what a unit costs beside its rows, in blocks
+constexpr int kMinShare = 2;                           // of a CTA's part of the line: at least one block of a unit
+// What is in shared memory behind the ring.
+struct Tail {
+  float part[kStreamWarps][kMaxG][kStride];            // of the warps, at the end of a unit
+  unsigned long long full[kSlots], empty[kSlots];
+  long long scan[kStreamWarps + 1], unit0;             // unit0: where the first unit of this CTA begins on the line
+  int b, h, abort, last;
+};
+constexpr int kSmemBytes = kSlots * kSlotBytes + sizeof(Tail);
+static_assert(2 * (kSmemBytes + 1024) <= 228 * 1024, "two CTAs to an SM (and no static shared memory: the ring begins at a multiple of 1024)");
+static_assert(kCtas <= kPagedMaxCtas, "");
 constexpr long long kWaitLimitCycles = 2000000000ll;   // about a second: a wait this long has failed
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
@@ -67,36 +80,33 @@ struct KernelArgs {
   float* lse;
   unsigned* counters;
   float* parts;                // [CTA][2][8][kStride]
-  const PagedTile* tokens;     // partial rows of the shared prefix, per sequence; null: none
+  const PagedToken* tokens;     // partial rows of the shared prefix, per sequence; null: none
   const float* prefix_rows;
+  long long max_rows;
   int box_rows, lg_box;
 };
 
 template <bool kF16>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const KernelArgs a) {
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long s_full[kSlots], s_empty[kSlots];
-  __shared__ long long s_scan[kStreamWarps + 1];
-  __shared__ long long s_unit0;      // where the first unit of this CTA begins on the line
-  __shared__ int s_b, s_h, s_blk;
-  __shared__ int s_abort;
-  __shared__ int s_last;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Tail& tail = *reinterpret_cast<Tail*>(smem + kSlots * kSlotBytes);
 
   const PagedGeom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  float* const wo = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + kSlots * kSlotBytes);
-  volatile int* abort_flag = &s_abort;
+  const uint32_t ring = smem_u32(smem);
+  volatile int* abort_flag = &tail.abort;
+  auto full = [&](int s) { return smem_u32(&tail.full[s]); };
+  auto empty = [&](int s) { return smem_u32(&tail.empty[s]); };
 
   pdl_trigger();
   if (tid == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      tc::mbar_init(smem_u32(&s_full[s]), 1);
-      tc::mbar_init(smem_u32(&s_empty[s]), kStreamWarps / 2);
+      tc::mbar_init(full(s), 1);
+      tc::mbar_init(empty(s), kStreamWarps);
     }
     tc::fence_mbar_init();
-    s_abort = 0;
+    tail.abort = 0;
   }
   if (tid == kStreamWarps * 32) {
     tc::tma_prefetch_desc(&k_map);
@@ -105,63 +115,77 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   pdl_wait();
 
   const int cap = g.max_pages << g.lg_page;
-  auto view_of = [&](int b) {
-    const int kv = __ldg(a.kv_len + b);
-    return paged_view<kLgRows>(min(max(kv, 0), cap), g.window, g.n_sink);
-  };
+  auto view = [&](int kv) { return paged_view<kLgRows>(min(max(kv, 0), cap), g.window, g.n_sink); };
+  auto length_of = [&](int b) { return b < g.B ? __ldg(a.kv_len + b) : 0; };
 
-  // ---- the line of blocks: its length, and the sequence, head and block at this CTA's start
+  // ---- the line: its length, and the unit at this CTA's start.  A unit's blocks come behind kUnitCost places without rows.
   long long total = 0;
-  auto scan = [&](int base, long long& incl, int& nb) {   // inclusive sums over the sequences base + tid; their sum
+  auto scan = [&](int base, long long& incl, int& places) {   // inclusive sums over the sequences base + tid; their sum
     const int b = base + tid;
-    nb = 0;
+    places = 0;
     if (b < g.B) {
-      const int kv = __ldg(a.kv_len + b);
+      const int kv = length_of(b);
       if ((kv < 0 || kv > cap) && blockIdx.x == 0) paged_flag(g.status, kBadLength);
-      nb = paged_view<kLgRows>(min(max(kv, 0), cap), g.window, g.n_sink).n_blocks;
+      places = view(kv).n_blocks + kUnitCost;
     }
-    incl = nb;
+    incl = places;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
     __syncthreads();
-    if (lane == 31) s_scan[warp] = incl;
+    if (lane == 31) tail.scan[warp] = incl;
     __syncthreads();
     long long all = 0;
 #pragma unroll
     for (int w = 0; w <= kStreamWarps; ++w) {
-      const long long v = s_scan[w];
+      const long long v = tail.scan[w];
       if (w < warp) incl += v;
       all += v;
     }
     return all;
   };
   long long incl = 0;
-  int nb0 = 0;
-  for (int base = 0; base < g.B; base += kThreads) total += scan(base, incl, nb0);
+  int places = 0;
+  for (int base = 0; base < g.B; base += kThreads) total += scan(base, incl, places);
   const long long line = total * g.Hkv;
-  const long long share = max((line + gridDim.x - 1) / gridDim.x, (long long)kMinBlocks);
+  const long long share = max((line + gridDim.x - 1) / gridDim.x, (long long)kMinShare);
   const long long begin = blockIdx.x * share, end = min(line, begin + share);
   if (begin >= line) return;
   long long before = 0;
   for (int base = 0; base < g.B; base += kThreads) {
-    const long long all = g.B > kThreads ? scan(base, incl, nb0) : total;
-    const long long u0 = (before + incl - nb0) * g.Hkv;
-    if (nb0 && begin >= u0 && begin < u0 + (long long)nb0 * g.Hkv) {
-      const long long rem = begin - u0;
-      s_b = base + tid;
-      s_h = (int)(rem / nb0);
-      s_blk = (int)(rem % nb0);
-      s_unit0 = u0 + (long long)s_h * nb0;
+    const long long all = g.B > kThreads ? scan(base, incl, places) : total;
+    const long long u0 = (before + incl - places) * g.Hkv;
+    if (places && begin >= u0 && begin < u0 + (long long)places * g.Hkv) {
+      const long long h = (begin - u0) / places;
+      tail.b = base + tid;
+      tail.h = (int)h;
+      tail.unit0 = u0 + h * places;
     }
     before += all;
   }
   __syncthreads();
-  int b = s_b, h = s_h, blk = s_blk;
-  long long unit0 = s_unit0, at = begin;     // the unit's begin and this role's place on the line
-  PagedView v = view_of(b);
+  int b = tail.b, h = tail.h;
+  long long unit0 = tail.unit0;
+  PagedView v = view(length_of(b));
+  int kv_next = length_of(b + 1);
+  // The unit's blocks [blk, blk + n) lie in this CTA's part.
+  auto segment = [&](int& blk) {
+    const long long first = unit0 + kUnitCost, lo = max(begin, first);
+    blk = (int)(lo - first);
+    return (int)max(0ll, min(end, first + v.n_blocks) - lo);
+  };
+  auto next_unit = [&]() {
+    unit0 += v.n_blocks + kUnitCost;
+    if (++h == g.Hkv) {
+      h = 0;
+      ++b;
+      v = view(kv_next);
+      kv_next = length_of(b + 1);
+    }
+    return unit0 < end;
+  };
 
   if (warp == kStreamWarps) {
     // ---------------------------------------------------------------- producer
@@ -171,77 +195,85 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     const uint32_t box_bytes = (uint32_t)a.box_rows * kRowBytes;
     int ids = 0, ids_at = -1, ids_b = -1;                   // lane i holds the page of rows (ids_at + i) * page.. of sequence ids_b
     int slot = 0;
-    uint32_t ph = 0;
-    for (; at < end; ++at) {
-      const int row0 = v.block(blk) << kLgRows;
-      const int pg = row0 >> g.lg_page, pg_last = (row0 + kSlotRows - 1) >> g.lg_page;
-      if (ids_b != b || pg < ids_at || pg_last >= ids_at + 32) {
-        ids_b = b;
-        ids_at = pg;
-        ids = pg + lane < g.max_pages ? __ldg(a.block_table + (size_t)b * g.max_pages + pg + lane) : -1;
-      }
-      const int r = row0 + (lane << a.lg_box);
-      const bool need = lane < boxes && r < v.kv && (r + a.box_rows > v.lo || r < g.n_sink);
-      int page = __shfl_sync(0xffffffffu, ids, ((r >> g.lg_page) - ids_at) & 31);
-      if (need && (page < 0 || page >= g.n_pages)) {
-        paged_flag(g.status, kBadPage);
-        page = g.n_pages;                                   // outside the pool: the copy brings zeros
-      }
-      const int n = __popc(__ballot_sync(0xffffffffu, need));
-      const uint32_t full = smem_u32(&s_full[slot]);
-      if (!wait_bounded(smem_u32(&s_empty[slot]), ph ^ 1u, abort_flag, g.status)) break;
-      if (lane == 0) tc::mbar_arrive_expect_tx(full, 2u * box_bytes * (uint32_t)n);
-      __syncwarp();
-      if (need) {
-        const uint32_t dst = ring + slot * kSlotBytes + (uint32_t)lane * box_bytes;
-        const int in_page = r & (g.page - 1);
-        tma_load_5d(dst, &k_map, full, 0, in_page, h, page, 0, pol);
-        tma_load_5d(dst + kPartBytes, &v_map, full, 0, in_page, h, page, 0, pol);
-      }
-      if (++slot == kSlots) { slot = 0; ph ^= 1u; }
-      if (++blk == v.n_blocks) {
-        blk = 0;
-        if (++h == g.Hkv) {
-          h = 0;
-          if (++b < g.B) v = view_of(b);
+    uint32_t ph = 1;
+    bool ok = true;
+    do {
+      int blk;
+      const int n = segment(blk);
+      for (int i = 0; ok && i < n; ++i) {
+        const int row0 = v.block(blk + i) << kLgRows;
+        const int pg = row0 >> g.lg_page, pg_last = (row0 + kSlotRows - 1) >> g.lg_page;
+        if (ids_b != b || pg < ids_at || pg_last >= ids_at + 32) {
+          ids_b = b;
+          ids_at = pg;
+          ids = pg + lane < g.max_pages ? __ldg(a.block_table + (size_t)b * g.max_pages + pg + lane) : -1;
         }
+        const int r = row0 + (lane << a.lg_box);
+        const bool need = lane < boxes && r < v.kv && (r + a.box_rows > v.lo || r < g.n_sink);
+        int page = __shfl_sync(0xffffffffu, ids, ((r >> g.lg_page) - ids_at) & 31);
+        if (need && (page < 0 || page >= g.n_pages)) {
+          paged_flag(g.status, kBadPage);
+          page = g.n_pages;                                   // outside the pool: the copy brings zeros
+        }
+        const int n_boxes = __popc(__ballot_sync(0xffffffffu, need));
+        ok = __all_sync(0xffffffffu, wait_bounded(empty(slot), ph, abort_flag, g.status));
+        if (!ok) break;
+        if (lane == 0) tc::mbar_arrive_expect_tx(full(slot), 2u * box_bytes * (uint32_t)n_boxes);
+        __syncwarp();
+        if (need) {
+          const uint32_t dst = ring + slot * kSlotBytes + (uint32_t)lane * box_bytes;
+          const int in_page = r & (g.page - 1);
+          tma_load_5d(dst, &k_map, full(slot), 0, in_page, h, page, 0, pol);
+          tma_load_5d(dst + kPartBytes, &v_map, full(slot), 0, in_page, h, page, 0, pol);
+        }
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
       }
-    }
+    } while (next_unit());
     return;
   }
 
   // ------------------------------------------------------------------ stream warps
   constexpr float kBias = kF16 ? 12.f : 0.f;   // (see pack16)
   const int gq = lane >> 2, tq = lane & 3;     // MMA fragment coordinates
-  const int group = warp >> 2, sub = warp & 3;
   const int mid = lane >> 3;
   const uint32_t plane = (uint32_t)a.box_rows * 128u;   // from the first half of a box's columns to the second
   // this warp's 16 rows of a slot
-  const uint32_t blk_off = (uint32_t)((sub * 16) >> a.lg_box) * 2u * plane + (uint32_t)((sub * 16) & (a.box_rows - 1)) * 128u;
+  const uint32_t blk_off = (uint32_t)((warp * 16) >> a.lg_box) * 2u * plane + (uint32_t)((warp * 16) & (a.box_rows - 1)) * 128u;
   auto off = [&](int row, int chunk) { return (uint32_t)(chunk >> 3) * plane + (uint32_t)(row * 128 + (((chunk & 7) ^ (row & 7)) << 4)); };
   auto load_q = [&](int b, int h, uint32_t (&qa)[kD / 16][2]) {
     const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q) + ((size_t)b * g.q_stride + (size_t)(h * g.G + min(gq, g.G - 1)) * kD) / 2 + tq;
 #pragma unroll
     for (int kk = 0; kk < kD / 16; ++kk) { qa[kk][0] = __ldg(src + kk * 8); qa[kk][1] = __ldg(src + kk * 8 + 4); }
   };
+  auto meet = [&]() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory"); };
 
-  uint32_t fill = 0;            // ring fills ahead of this role's place
-  while (at < end) {
-    const int seg = (int)min(end - at, (long long)(v.n_blocks - blk));
+  uint32_t q_next[kD / 16][2];     // the next unit's queries are on their way while this one streams
+  load_q(b, h, q_next);
+  int slot = 0;
+  uint32_t ph = 0;
+  do {
+    int blk;
+    const int n_blk = segment(blk);
     uint32_t qa[kD / 16][2];
-    load_q(b, h, qa);
+#pragma unroll
+    for (int kk = 0; kk < kD / 16; ++kk) { qa[kk][0] = q_next[kk][0]; qa[kk][1] = q_next[kk][1]; }
+    {
+      const bool wrap = h + 1 == g.Hkv;
+      load_q(min(b + (wrap ? 1 : 0), g.B - 1), wrap ? 0 : h + 1, q_next);
+    }
+    if (n_blk == 0) continue;
+    int4 prefix = make_int4(0, 0, 0, 0);
+    if (a.tokens) prefix = __ldg(reinterpret_cast<const int4*>(a.tokens) + b);   // {row, chunks, rows to the next chunk, and to the next head}
     float o[kD / 16][4];
 #pragma unroll
     for (int n = 0; n < kD / 16; ++n) { o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f; }
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // heads 2tq and 2tq+1
 
-    for (int i = (int)((fill ^ (uint32_t)group) & 1u); i < seg; i += 2) {
-      const uint32_t f = fill + (uint32_t)i;
-      const int s = (int)(f % kSlots);
-      const int r0 = (v.block(blk + i) << kLgRows) + sub * 16;
-      const bool ok = wait_bounded(smem_u32(&s_full[s]), (f / kSlots) & 1u, abort_flag, g.status);
+    for (int i = 0; i < n_blk; ++i) {
+      const int r0 = (v.block(blk + i) << kLgRows) + warp * 16;
+      const bool ok = wait_bounded(full(slot), ph, abort_flag, g.status);
       if (ok && r0 < v.kv && (r0 + 16 > v.lo || r0 < g.n_sink)) {
-        const uint32_t sK = ring + s * kSlotBytes + blk_off, sV = sK + kPartBytes;
+        const uint32_t sK = ring + slot * kSlotBytes + blk_off, sV = sK + kPartBytes;
         float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};   // two accumulators halve the chain
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
@@ -288,16 +320,18 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
       }
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(smem_u32(&s_empty[s]));
+      if (lane == 0) tc::mbar_arrive(empty(slot));
+      if (++slot == kSlots) { slot = 0; ph ^= 1u; }
     }
 #pragma unroll
     for (int w = 4; w < 32; w <<= 1) {
       l0 += __shfl_xor_sync(0xffffffffu, l0, w);
       l1 += __shfl_xor_sync(0xffffffffu, l1, w);
     }
-    // ---- the eight warps' partials, then a warp per head with four outputs a lane
+    // ---- the warps' partials, then a warp per head with four outputs a lane
+    meet();                        // (those of the unit before have been read)
     if (2 * tq < g.G) {
-      float* w0 = wo + (warp * kMaxG + 2 * tq) * kStride;
+      float* w0 = tail.part[warp][2 * tq];
 #pragma unroll
       for (int n = 0; n < kD / 16; ++n) {
         w0[n * 16 + gq] = o[n][0]; w0[n * 16 + gq + 8] = o[n][2];
@@ -308,77 +342,72 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         w0[kStride + kD] = m1; w0[kStride + kD + 1] = l1;
       }
     }
-    asm volatile("barrier.cta.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");
-    Partial p;
-    p.o[0] = p.o[1] = p.o[2] = p.o[3] = 0.f; p.m = -INFINITY; p.l = 0.f;
-    if (warp < g.G) {
+    meet();
+    auto own = [&](int head) {
+      Partial p;
+      p.clear();
       float mw[kStreamWarps];
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) { mw[w] = wo[(w * kMaxG + warp) * kStride + kD]; p.m = fmaxf(p.m, mw[w]); }
+      for (int w = 0; w < kStreamWarps; ++w) { mw[w] = tail.part[w][head][kD]; p.m = fmaxf(p.m, mw[w]); }
       const float ref = p.m == -INFINITY ? 0.f : p.m;
 #pragma unroll
       for (int w = 0; w < kStreamWarps; ++w) {
-        const float* r = wo + (w * kMaxG + warp) * kStride;
+        const float* r = tail.part[w][head];
         const float f = ex2_approx(mw[w] - ref);
         const float4 x = *reinterpret_cast<const float4*>(r + 4 * lane);
         p.l = fmaf(r[kD + 1], f, p.l);
         p.o[0] = fmaf(x.x, f, p.o[0]); p.o[1] = fmaf(x.y, f, p.o[1]);
         p.o[2] = fmaf(x.z, f, p.o[2]); p.o[3] = fmaf(x.w, f, p.o[3]);
       }
-    }
-    const int c_first = (int)(unit0 / share), c_last = (int)((unit0 + v.n_blocks - 1) / share);
-    bool finish = true;
-    if (c_first != c_last) {
-      if (warp < g.G) {
-        float* r = a.parts + (((size_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * kMaxG + warp) * kStride;
-        __stcg(reinterpret_cast<float4*>(r) + lane, make_float4(p.o[0], p.o[1], p.o[2], p.o[3]));
-        if (lane == 0) __stcg(reinterpret_cast<float2*>(r + kD), make_float2(p.m, p.l));
-        __threadfence();
-      }
-      asm volatile("barrier.cta.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");
-      if (tid == 0) {
-        const unsigned n = atomicAdd(a.counters + c_first, 1u);
-        const bool last = n == (unsigned)(c_last - c_first);
-        if (last) a.counters[c_first] = 0u;     // everybody has arrived: ready for the next launch
-        __threadfence();
-        s_last = last;
-      }
-      asm volatile("barrier.cta.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");
-      finish = s_last != 0;
-      if (finish && warp < g.G) {
-        p.o[0] = p.o[1] = p.o[2] = p.o[3] = 0.f; p.m = -INFINITY; p.l = 0.f;
-        join_rows(p, c_last - c_first + 1, lane, [&](int i) {
-          return a.parts + (((size_t)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * kMaxG + warp) * kStride;
-        });
-      }
-    }
-    if (finish && warp < g.G) {
-      if (a.tokens) {
-        const int4 t = __ldg(reinterpret_cast<const int4*>(a.tokens) + b);   // {row, chunks, rows of a head, -}
-        join_rows(p, t.y, lane, [&](int i) { return a.prefix_rows + ((size_t)t.x + ((size_t)i * g.Hkv + h) * t.z + warp) * kStride; });
-      }
-      const int hq = h * g.G + warp;
+      return p;
+    };
+    auto finish = [&](Partial& p, int head) {
+      const long long last_row = prefix.x + (long long)(prefix.y - 1) * prefix.z + (long long)h * prefix.w + head;
+      if (prefix.y > 0 && prefix.x >= 0 && prefix.z >= 0 && prefix.w >= 0 && last_row < a.max_rows)   // (not so only after a group_start that falls)
+        join_rows(p, prefix.y, lane, [&](int i) { return a.prefix_rows + ((size_t)prefix.x + (size_t)i * prefix.z + (size_t)h * prefix.w + head) * kStride; });
+      const int hq = h * g.G + head;
       const float inv = p.l == 0.f ? 0.f : 1.f / p.l;    // no visible row: zeros
       uint2 w;
       w.x = pack16<kF16>(p.o[0] * inv, p.o[1] * inv);
       w.y = pack16<kF16>(p.o[2] * inv, p.o[3] * inv);
       reinterpret_cast<uint2*>(a.out)[((size_t)b * g.Hq + hq) * (kD / 4) + lane] = w;
       if (a.lse && lane == 0) a.lse[(size_t)b * g.Hq + hq] = p.l == 0.f ? -INFINITY : (p.m + log2f(p.l)) * kLn2;
-    }
-    asm volatile("barrier.cta.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");   // the partials may be overwritten
-
-    at += seg;
-    fill += (uint32_t)seg;
-    blk += seg;
-    if (blk == v.n_blocks) {
-      unit0 += v.n_blocks;
-      blk = 0;
-      if (++h == g.Hkv) {
-        h = 0;
-        if (++b < g.B) v = view_of(b);
+    };
+    const long long first = unit0 + kUnitCost;
+    if (first >= begin && first + v.n_blocks <= end) {
+      for (int head = warp; head < g.G; head += kStreamWarps) {
+        Partial p = own(head);
+        finish(p, head);
       }
+    } else {
+      const int c_first = (int)(first / share), c_last = (int)((first + v.n_blocks - 1) / share);
+      for (int head = warp; head < g.G; head += kStreamWarps) {
+        const Partial p = own(head);
+        float* r = a.parts + (((size_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * kMaxG + head) * kStride;
+        __stcg(reinterpret_cast<float4*>(r) + lane, make_float4(p.o[0], p.o[1], p.o[2], p.o[3]));
+        if (lane == 0) __stcg(reinterpret_cast<float2*>(r + kD), make_float2(p.m, p.l));
+      }
+      __threadfence();
+      meet();
+      if (tid == 0) {
+        const unsigned n = atomicAdd(a.counters + c_first, 1u);
+        const bool last = n == (unsigned)(c_last - c_first);
+        if (last) a.counters[c_first] = 0u;     // everybody has arrived: ready for the next launch
+        __threadfence();
+        tail.last = last;
+      }
+      meet();
+      if (*reinterpret_cast<volatile int*>(&tail.last))
+        for (int head = warp; head < g.G; head += kStreamWarps) {
+          Partial p;
+          p.clear();
+          join_rows(p, c_last - c_first + 1, lane, [&](int i) {
+            return a.parts + (((size_t)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * kMaxG + head) * kStride;
+          });
+          finish(p, head);
+        }
     }
-  }
+  } while (next_unit());
 }
 
 template <bool kF16>
@@ -391,13 +420,14 @@ cudaError_t launch(const PagedDecodeArgs& d, const PagedWs& ws, cudaStream_t st)
   a.q = d.q; a.block_table = d.block_table; a.kv_len = d.kv_len; a.out = d.out; a.lse = d.lse;
   a.counters = (unsigned*)(d.wsp + kPagedCounters);
   a.parts = (float*)(d.wsp + kPagedDecodeParts);
-  a.tokens = d.n_groups ? (const PagedTile*)(d.wsp + ws.tiles) : nullptr;
+  a.tokens = d.n_groups ? (const PagedToken*)(d.wsp + ws.tokens) : nullptr;
   a.prefix_rows = (const float*)(d.wsp + ws.part_o);
+  a.max_rows = ws.max_rows;
   a.box_rows = std::min(d.g.page, kSlotRows);
   while ((1 << a.lg_box) < a.box_rows) ++a.lg_box;
   CUtensorMap km, vm;
   if (!paged_kv_map(&km, d.K, d.g, a.box_rows, 2) || !paged_kv_map(&vm, d.V, d.g, a.box_rows, 2)) return cudaErrorInvalidValue;
-  e = launch_pdl(paged_decode_kernel<kF16>, dim3(kSms), dim3(kThreads), kSmemBytes, st, km, vm, a);
+  e = launch_pdl(paged_decode_kernel<kF16>, dim3(kCtas), dim3(kThreads), kSmemBytes, st, km, vm, a);
   if (e == cudaSuccess) count_launch(1);
   return e;
 }

@@ -3,11 +3,13 @@
 //
 //   S = Q K^T,  P = exp2(scale2 S - m),  O = sum P V,  l = sum P;  out = O / l,  lse = (m + log2 l) ln 2
 //
-// An item is up to 256 query rows of a (sequence, kv head), tokens times the G heads of the group, so that a tile of K and V
-// serves the whole group, against a range of steps, each a tile of 128 keys.  paged_plan_kernel makes the list of items from the
-// lengths, which are on the device; items that are long against the mean share of an SM are cut along the keys (few tokens on a long
-// cache), and the list is in falling order of cost, dealt to the persistent CTAs forwards and backwards in turn.  What was cut is
-// joined by paged_combine_kernel, or by the decode kernel.
+// A tile is up to 256 query rows of a (sequence, kv head), tokens times the G heads of the group, so that a tile of K and V serves
+// the whole group; its work is a number of steps, each 128 keys.  The lengths are on the device and may be anything, so the work is
+// dealt there: every CTA sums the steps of all tiles, lists the heavy ones (half an SM's mean share or more: few) from the
+// heaviest down, cuts those of twice the share or more along the keys, and takes one piece after another from a common counter, the
+// heavy tiles ahead of the others, which come sequence by sequence, the last tokens (which see the most keys) first.  Of a tile that is
+// cut each CTA leaves partial rows and the last to arrive joins them, in the order of the keys; those of a shared prefix are
+// joined by the decode kernel.
 //
 // A CTA works on two streams of 128 rows; while one stream has its softmax the other has the tensor cores.  A stream is two
 // warpgroups, two threads to a row, 64 of a tile's keys each.  Tensor memory: S of the streams at columns 0 and 128, O at 256 and
@@ -32,238 +34,116 @@ namespace {
 using namespace tc;
 
 constexpr int kSoftmaxWarps = 16;                 // two streams of two warpgroups
-constexpr int kProducerWarp = 16, kMmaWarp = 17, kQWarp = 18;
+constexpr int kProducerWarp = 16, kMmaWarp = 17, kQWarp = 18, kSchedWarp = 19;
 constexpr int kThreads = 640;
 constexpr int kSlots = 5;                         // K and V tiles in one ring, in the order in which they are used
 constexpr int kTileBytes = kKvTileBytes;          // 32 KB
+constexpr uint32_t kColO = 256;
+constexpr int kMaxHeavy = 2 * kSms;               // tiles of at least half an SM's mean share
+constexpr int kItemReaders = kSoftmaxWarps + 3;   // warps that take a piece from the scheduler
+
+// A piece of work: a tile of rows of one kv head against a range of steps.
+struct Piece {
+  int tok0, n_tok;       // its tokens
+  int seq;               // whose row of the block table
+  int head;              // kv head
+  int pos0;              // position of the first token
+  int kv_end;            // keys at and beyond it are seen by none of the tokens
+  int win_lo;            // keys in [n_sink, win_lo) neither
+  int near_tiles, skip;  // step j is tile j, or j + skip from step near_tiles on
+  int step0, n_steps;    // n_steps 0: there is no more work
+  int part_row;          // of a tile that is cut, its first partial row for this head and chunk; or -1
+  int part_step;         // rows from a chunk's partial rows to the next chunk's
+  int n_chunks, counter; // chunks, and which arrival counter of them
+  int chunk_steps;
+};
+static_assert(sizeof(Piece) == 64, "four 16-byte vectors");
+
+// A heavy tile.
+struct Heavy {
+  int seq, t;            // tile t of a sequence
+  int n_chunks, chunk_steps;
+  int first_piece;       // chunks ahead of its own, over the list
+  int part_row;          // first partial row, if it is cut
+  int counter;           // first arrival counter, if it is cut
+  int pad;
+};
+
 // What is in shared memory beside the two query blocks and the ring.
 struct Tail {
-  unsigned long long bars[2 * kSlots + 12];
+  unsigned long long bars[3 * kSlots + 16];
+  Piece piece[2];
   float max[2][2][128];                           // [stream][half][row]: maxima of a tile's halves, and at the end the sums
   uint32_t tmem;
+  int last[2];
   Ctl ctl;
 };
 constexpr int kSmemBytes = (2 + kSlots) * kTileBytes + sizeof(Tail);
 static_assert(kSmemBytes <= 227 * 1024, "all of it: there is no static shared memory, so that the tiles begin at a multiple of 1024");
-constexpr uint32_t kColO = 256;
-constexpr int kPlanThreads = 1024;
-constexpr int kBuckets = 256;
-
-struct PlanArgs {
-  PagedGeom g;
-  const int *q_start, *kv_len;
-  int n_seqs, causal, partial, grid;
-  int item_tokens;                // tokens of an item: 2 * (128 / G)
-  PagedPlanHeader* head;
-  PagedItem* items;
-  PagedTile* tiles;
-  int max_tiles, max_items, max_split;
-  long long max_rows;
-};
-
-// 0..255, growing with c: eight steps to a factor of two
-__device__ __forceinline__ int cost_bucket(int c) {
-  if (c < 16) return c;
-  const int lg = 31 - __clz(c);
-  return min(kBuckets - 1, (lg - 3) * 8 + 8 + ((c >> (lg - 3)) & 7));
-}
-
-__global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PlanArgs a) {
-  __shared__ int tb[kMaxSequences + 1];      // first tile of each sequence
-  __shared__ int warp_sum[32];
-  __shared__ unsigned long long s_steps;
-  __shared__ int s_hist[kBuckets];
-  __shared__ unsigned long long s_rows;
-  __shared__ int s_split, s_carry;
-  const PagedGeom& g = a.g;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  pdl_trigger();
-  if (tid == 0) { s_steps = 0; s_rows = 0; s_split = 0; s_carry = 0; }
-  if (tid < kBuckets) s_hist[tid] = 0;
-  pdl_wait();
-  const int cap = g.max_pages << g.lg_page;
-  auto lengths = [&](int b, int& s0, int& n, int& kv) {
-    s0 = __ldg(a.q_start + b);
-    const int s1 = __ldg(a.q_start + b + 1);
-    kv = __ldg(a.kv_len + b);
-    const bool bad = s0 < 0 || s1 < s0 || s1 > g.n_tokens;
-    n = bad ? 0 : s1 - s0;
-    const bool bad_kv = kv < 0 || kv > cap;
-    kv = min(max(kv, 0), cap);
-    return bad || bad_kv;
-  };
-  // tiles of the sequences
-  for (int base = 0; base < a.n_seqs; base += kPlanThreads) {
-    const int b = base + tid;
-    int nt = 0;
-    if (b < a.n_seqs) {
-      int s0, n, kv;
-      if (lengths(b, s0, n, kv)) paged_flag(g.status, kBadLength);
-      nt = (n + a.item_tokens - 1) / a.item_tokens;
-    }
-    int incl = nt;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    __syncthreads();
-    if (lane == 31) warp_sum[warp] = incl;
-    __syncthreads();
-    if (warp == 0) {
-      int v = warp_sum[lane];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
-      }
-      warp_sum[lane] = v;
-    }
-    __syncthreads();
-    const int carry = s_carry;
-    incl += carry + (warp ? warp_sum[warp - 1] : 0);
-    if (b < a.n_seqs) tb[b + 1] = min(incl, a.max_tiles);   // (more than that only with a q_start that falls)
-    __syncthreads();
-    if (tid == 0) s_carry = min(carry + warp_sum[31], a.max_tiles);
-  }
-  if (tid == 0) tb[0] = 0;
-  if (a.partial)
-    for (int t = tid; t < g.n_tokens; t += kPlanThreads) a.tiles[t] = PagedTile{0, 0, 0, 0};
-  __syncthreads();
-  const int n_tiles = tb[a.n_seqs];
-  auto tile_of = [&](int e, PagedItem& it) {
-    int lo = 0, hi = a.n_seqs;             // tb[lo] <= e < tb[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tb[mid] <= e) lo = mid; else hi = mid;
-    }
-    int s0, n, kv;
-    lengths(lo, s0, n, kv);
-    const int t = e - tb[lo], first_tok = t * a.item_tokens;
-    it.seq = lo;
-    it.tok0 = s0 + first_tok;
-    it.n_tok = min(a.item_tokens, n - first_tok);
-    it.pos0 = a.causal ? kv - n + first_tok : 1 << 30;
-    it.kv_end = a.causal ? max(0, min(kv, it.pos0 + it.n_tok)) : kv;
-    it.win_lo = a.causal && g.window ? max(0, it.pos0 - g.window + 1) : 0;
-    const int last = (it.kv_end + kPagedTileKeys - 1) / kPagedTileKeys, first = min(it.win_lo / kPagedTileKeys, last);
-    it.near_tiles = (int)min((long long)first, ((long long)g.n_sink + kPagedTileKeys - 1) / kPagedTileKeys);
-    it.skip = first - it.near_tiles;
-    it.step0 = 0;
-    it.n_steps = max(1, it.near_tiles + last - first);
-    it.part_row = -1;
-    it.rows = it.n_tok * g.G;
-  };
-  // how much work there is
-  unsigned long long steps = 0;
-  for (int e = tid; e < n_tiles; e += kPlanThreads) {
-    PagedItem it;
-    tile_of(e, it);
-    steps += (unsigned)it.n_steps;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
-  if (lane == 0 && steps) atomicAdd(&s_steps, steps);
-  __syncthreads();
-  const unsigned long long all = s_steps * (unsigned long long)g.Hkv;
-  // A tile of rows is cut into as many chunks as it has times the mean share of an SM, rounded down: all chunks of cut tiles together are no more than the
-  // SMs, and tiles of less than twice the share stay whole.
-  auto chunks_of = [&](const PagedItem& it) {
-    const unsigned long long k = (unsigned long long)it.n_steps * a.grid / all;
-    return (int)max(1ull, min(k, (unsigned long long)it.n_steps));
-  };
-  for (int e = tid; e < n_tiles; e += kPlanThreads) {
-    PagedItem it;
-    tile_of(e, it);
-    const int k = chunks_of(it), len = (it.n_steps + k - 1) / k;
-    atomicAdd(&s_hist[cost_bucket(len)], (it.n_steps + len - 1) / len);
-  }
-  __syncthreads();
-  if (warp == 0) {      // places of the buckets in the list, the costliest first
-    int carry = 0;
-    for (int base = kBuckets - 32; base >= 0; base -= 32) {
-      const int i = base + 31 - lane, n = s_hist[i];
-      int incl = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += u;
-      }
-      s_hist[i] = carry + incl - n;
-      carry += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) { a.head->n_items = min(carry, a.max_items); a.head->n_tiles = n_tiles; }
-  }
-  __syncthreads();
-  for (int e = tid; e < n_tiles; e += kPlanThreads) {
-    PagedItem it;
-    tile_of(e, it);
-    int k = chunks_of(it);
-    const int len = (it.n_steps + k - 1) / k;
-    k = (it.n_steps + len - 1) / len;
-    const int slot = atomicAdd(&s_hist[cost_bucket(len)], k);
-    const bool parts = a.partial || k > 1;
-    int row = -1;
-    if (parts) {
-      // (which rows a tile gets is a matter of who comes first; what is written there is not)
-      const unsigned long long at = atomicAdd(&s_rows, (unsigned long long)k * g.Hkv * it.rows);
-      if ((long long)(at + (unsigned long long)k * g.Hkv * it.rows) > a.max_rows) {
-        paged_flag(g.status, kBadLength);    // (cannot be, but for a q_start that falls)
-        row = -2;
-      } else {
-        row = (int)at;
-      }
-      if (!a.partial && row >= 0) {
-        const int i = atomicAdd(&s_split, 1);
-        if (i < a.max_split) a.tiles[i] = PagedTile{row, k, it.rows, it.tok0};
-      }
-      if (a.partial && row >= 0)
-        for (int i = 0; i < it.n_tok; ++i) a.tiles[it.tok0 + i] = PagedTile{row + i * g.G, k, it.rows, 0};
-    }
-    for (int c = 0; c < k; ++c) {
-      if (slot + c >= a.max_items) break;
-      PagedItem x = it;
-      x.step0 = c * len;
-      x.n_steps = min(len, it.n_steps - x.step0);
-      x.part_row = row < 0 ? row : row + c * g.Hkv * it.rows;
-      a.items[slot + c] = x;
-    }
-  }
-  __syncthreads();
-  if (tid == 0) a.head->n_split = min(s_split, a.max_split);
-}
+static_assert((kMaxSequences + 1 + 63) * 4 + kMaxHeavy * 16 <= kSlots * kTileBytes, "the list of work is made where the ring will be");
 
 struct KernelArgs {
   PagedGeom g;
-  const int* block_table;
-  const PagedPlanHeader* head;
-  const PagedItem* items;
+  const int *block_table, *q_start, *kv_len;
+  int n_seqs, causal, partial;
+  int tokens;                 // of a stream: 128 / G
+  int g_inv;                  // row / G = row * g_inv >> 16 for a row of a stream
+  int box_rows, lg_box;
+  unsigned* sched;            // [0] next piece, [1] CTAs that are done, then the arrival counters; all zero between launches
+  Heavy* heavy;               // a list for each CTA
+  PagedToken* token_parts;    // partial: where the decode kernel finds its rows
   float* parts;
+  long long max_rows;
   void* out;
   float* lse;
-  int tokens;                 // of a stream: 128 / G
-  int box_rows, lg_box;
 };
 
-__device__ __forceinline__ PagedItem load_item(const PagedItem* items, int e) {
-  PagedItem it;
-  const int4* s = reinterpret_cast<const int4*>(items + e);
-  int4* d = reinterpret_cast<int4*>(&it);
-  d[0] = __ldg(s); d[1] = __ldg(s + 1); d[2] = __ldg(s + 2);
-  return it;
+// Sequence b: its first token, number of tokens and cached rows, held to what the buffers allow.
+__device__ __forceinline__ bool lengths(const KernelArgs& a, int b, int& s0, int& n, int& kv) {
+  const int cap = a.g.max_pages << a.g.lg_page;
+  s0 = __ldg(a.q_start + b);
+  const int s1 = __ldg(a.q_start + b + 1);
+  kv = __ldg(a.kv_len + b);
+  const bool bad = s0 < 0 || s1 < s0 || s1 > a.g.n_tokens, bad_kv = kv < 0 || kv > cap;
+  n = bad ? 0 : s1 - s0;
+  kv = min(max(kv, 0), cap);
+  return bad || bad_kv;
 }
 
-// The CTA's items: of every `grid` places of the list the CTA's own, from the front and from the back in turn.
-struct Deal {
-  int round, n;
-  __device__ __forceinline__ explicit Deal(int n_) : round(0), n(n_) {}
-  __device__ __forceinline__ int next() {
-    const int i = (round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x;
-    const long long w = (long long)round * gridDim.x + i;
-    ++round;
-    return w < n ? (int)w : -1;
-  }
-};
+// Tile t of a sequence (the last tokens first), all of its steps.
+__device__ __forceinline__ void tile_piece(const KernelArgs& a, int seq, int s0, int n, int kv, int t, Piece& p) {
+  const PagedGeom& g = a.g;
+  const int size = 2 * a.tokens, n_tiles = (n + size - 1) / size;
+  const int first_tok = (n_tiles - 1 - t) * size;
+  p.seq = seq;
+  p.tok0 = s0 + first_tok;
+  p.n_tok = min(size, n - first_tok);
+  p.pos0 = a.causal ? kv - n + first_tok : 1 << 30;
+  p.kv_end = a.causal ? max(0, min(kv, p.pos0 + p.n_tok)) : kv;
+  p.win_lo = a.causal && g.window ? max(0, p.pos0 - g.window + 1) : 0;
+  const int last = (p.kv_end + kPagedTileKeys - 1) / kPagedTileKeys, first = min(p.win_lo / kPagedTileKeys, last);
+  p.near_tiles = (int)min((long long)first, ((long long)g.n_sink + kPagedTileKeys - 1) / kPagedTileKeys);
+  p.skip = first - p.near_tiles;
+  p.step0 = 0;
+  p.n_steps = max(1, p.near_tiles + last - first);
+  p.part_row = -1; p.part_step = 0; p.n_chunks = 1; p.counter = 0; p.chunk_steps = 1;
+}
+
+// Half the mean share of an SM or more.
+__device__ __forceinline__ bool is_heavy(int n, unsigned long long all) { return 2ull * n * gridDim.x >= all; }
+
+// Into how many chunks a tile of n steps is cut, `all` being the steps of all tiles and heads.  Twice the mean share of an SM or more is cut into as many
+// pieces as it has shares, so that all pieces of cut tiles together are no more than the SMs.  Joining k chunks of `rows` rows costs the
+// last CTA about 8 cycles a row and chunk, and a chunk less takes n / k steps of 3000 cycles off: beyond sqrt(375 n / rows) chunks
+// the joining costs more than it gives (a shared prefix is joined elsewhere, by many).
+__device__ __forceinline__ int chunks_of(const KernelArgs& a, int n, int rows, unsigned long long all) {
+  const unsigned long long shares = (unsigned long long)n * gridDim.x / all;
+  if (shares < 2) return 1;
+  int k = (int)min(shares, (unsigned long long)n);
+  if (!a.partial) k = max(1, min(k, (int)sqrtf(375.f * n / rows)));
+  const int len = (n + k - 1) / k;
+  return (n + len - 1) / len;
+}
 
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -282,16 +162,20 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   auto q_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };
   auto q_empty = [&](int s) { return bar0 + 8u * (2 * kSlots + 2 + s); };
   auto s_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 4 + s); };
-  auto p_full = [&](int s, int part) { return bar0 + 8u * (2 * kSlots + 6 + (part ? 4 : 0) + s); };
-  auto o_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 8 + s); };
+  auto p_full = [&](int s, int part) { return bar0 + 8u * (2 * kSlots + 6 + 2 * part + s); };
+  auto o_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 10 + s); };
+  auto piece_full = [&](int i) { return bar0 + 8u * (2 * kSlots + 12 + i); };
+  auto piece_empty = [&](int i) { return bar0 + 8u * (2 * kSlots + 14 + i); };
+  auto clean = [&](int s) { return bar0 + 8u * (2 * kSlots + 16 + s); };   // the tile of V in the slot has had its unseen rows cleared
 
   if (tid == 0) {
     ctl.abort = 0;
     ctl.status = g.status;
-    for (int s = 0; s < kSlots; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < kSlots; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 2); mbar_init(clean(s), 1); }   // read by the MMAs, passed by the clearing warp
     for (int s = 0; s < 2; ++s) {
       mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1);
       mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 256); mbar_init(p_full(s, 1), 256); mbar_init(o_full(s), 1);
+      mbar_init(piece_full(s), 1); mbar_init(piece_empty(s), kItemReaders);
     }
     fence_mbar_init();
   }
@@ -307,10 +191,241 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   tc_fence_after_sync();
   const uint32_t tmem_base = tail.tmem;
   pdl_wait();
-  const int n_work = a.head->n_items * g.Hkv;
   const int R = a.tokens;
 
-  if (warp == kProducerWarp) {
+  // ---- the list of work, the same in every CTA: first tiles of the sequences, all steps, heavy tiles
+  int* const tb = reinterpret_cast<int*>(smem_al + 2 * kTileBytes);   // [n_seqs + 1], where the ring will be
+  int* const sums = tb + kMaxSequences + 1;                           // [32] and a count
+  int2* const found = reinterpret_cast<int2*>(sums + 63);             // [kMaxHeavy] {tile, steps}
+  Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
+  const int size = 2 * R;
+  auto block_sum = [&](int incl, int& before) {      // of inclusive warp sums: their total, and what lies ahead of this warp
+    __syncthreads();
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    int all = 0;
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      const int v = sums[w];
+      if (w < warp) before += v;
+      all += v;
+    }
+    return all;
+  };
+  int n_tiles = 0;
+  for (int base = 0; base < a.n_seqs; base += kThreads) {
+    const int b = base + tid;
+    int nt = 0;
+    if (b < a.n_seqs) {
+      int s0, n, kv;
+      if (lengths(a, b, s0, n, kv) && blockIdx.x == 0) paged_flag(g.status, kBadLength);
+      nt = (n + size - 1) / size;
+    }
+    int incl = nt, before;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const int all = block_sum(incl, before);
+    if (b < a.n_seqs) tb[b] = n_tiles + before + incl - nt;
+    n_tiles += all;
+  }
+  if (tid == 0) tb[a.n_seqs] = n_tiles;
+  if (a.partial)      // tokens of no group have no partial rows
+    for (int t = blockIdx.x * kThreads + tid; t < g.n_tokens; t += gridDim.x * kThreads)
+      if (t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs)) a.token_parts[t] = PagedToken{0, 0, 0, 0};
+  __syncthreads();
+  auto tile_of = [&](int e, Piece& p) {
+    int lo = 0, hi = a.n_seqs;             // tb[lo] <= e < tb[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tb[mid] <= e) lo = mid; else hi = mid;
+    }
+    int s0, n, kv;
+    lengths(a, lo, s0, n, kv);
+    tile_piece(a, lo, s0, n, kv, e - tb[lo], p);
+  };
+  unsigned long long steps = 0;
+  for (int e = tid; e < n_tiles; e += kThreads) {
+    Piece p;
+    tile_of(e, p);
+    steps += (unsigned)p.n_steps;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
+  unsigned long long* const wide = reinterpret_cast<unsigned long long*>(found);
+  if (lane == 0) wide[warp] = steps;
+  __syncthreads();
+  unsigned long long all_steps = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) all_steps += wide[w];
+  all_steps *= (unsigned long long)g.Hkv;
+  __syncthreads();
+  // heavy tiles, in the order of the tiles
+  int n_heavy = 0;
+  for (int base = 0; base < n_tiles; base += kThreads) {
+    const int e = base + tid;
+    Piece p;
+    bool is = false;
+    if (e < n_tiles) {
+      tile_of(e, p);
+      is = is_heavy(p.n_steps, all_steps);
+    }
+    if (!__syncthreads_or(is)) continue;
+    const unsigned m = __ballot_sync(0xffffffffu, is);
+    int before;
+    const int all = block_sum(__popc(m), before);
+    const int i = n_heavy + before + __popc(m & ((1u << lane) - 1u));
+    if (is && i < kMaxHeavy) found[i] = make_int2(e, 0);
+    n_heavy += all;
+  }
+  n_heavy = min(n_heavy, kMaxHeavy);   // (there are no more)
+  // ... the heaviest first
+  int n_heavy_pieces = 0;
+  if (n_heavy) {
+    __syncthreads();
+    int2* const order = found + kMaxHeavy;     // by rank: {chunks, rows of a head}
+    Piece p;
+    int k = 0, len = 0, rank = 0;
+    if (tid < n_heavy) {
+      tile_of(found[tid].x, p);
+      k = chunks_of(a, p.n_steps, p.n_tok * g.G, all_steps);
+      len = (p.n_steps + k - 1) / k;
+      found[tid].y = len;
+    }
+    __syncthreads();
+    if (tid < n_heavy) {
+      for (int j = 0; j < n_heavy; ++j) {
+        const int l = found[j].y;
+        rank += l > len || (l == len && j < tid);
+      }
+      order[rank] = make_int2(k, p.n_tok * g.G);
+    }
+    __syncthreads();
+    if (tid < n_heavy) {
+      Heavy x{p.seq, found[tid].x - tb[p.seq], k, len, 0, a.partial ? g.n_tokens * g.Hq : 0, 0, 0};
+      for (int j = 0; j < rank; ++j) {
+        const int2 o = order[j];
+        x.first_piece += o.x;
+        if (o.x > 1) { x.part_row += o.x * g.Hkv * o.y; x.counter += 2 * g.Hkv; }
+      }
+      heavy[rank] = x;
+    }
+    for (int j = 0; j < n_heavy; ++j) n_heavy_pieces += order[j].x;
+  }
+  fence_proxy_async_smem();    // the ring's copies come after what was written there
+  __syncthreads();
+
+  // The next piece of work; false: there is none, or a wait has run out.
+  uint32_t n_taken = 0;
+  auto take_piece = [&](Piece& p) {
+    const int i = n_taken & 1;
+    if (!__all_sync(0xffffffffu, mbar_wait_far(&ctl, piece_full(i), (n_taken >> 1) & 1u, 0x800u))) return false;
+    p = tail.piece[i];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(piece_empty(i));
+    ++n_taken;
+    return p.n_steps != 0;
+  };
+  auto step_row = [](const Piece& p, int j) { return (p.step0 + j < p.near_tiles ? p.step0 + j : p.step0 + j + p.skip) * kTileKeys; };
+  // whether a tile of keys has rows that none of the tokens sees
+  auto unseen_rows = [&](const Piece& p, int row0) {
+    return row0 + kTileKeys > p.kv_end || (row0 < p.win_lo && row0 + kTileKeys > g.n_sink);
+  };
+
+  if (warp == kSchedWarp) {
+    // ------------------------------------------------------------ scheduler: which piece is next, and what it is
+    const long long heavy_work = (long long)n_heavy_pieces * g.Hkv, total = heavy_work + (long long)n_tiles * g.Hkv;
+    long long w = blockIdx.x;
+    int at_heavy = 0;
+    int strip = -32, strip_first = 0, strip_all = 0, incl = 0, nt = 0, s0 = 0, n = 0, kv = 0;   // 32 sequences, one a lane
+    uint32_t n_given = 0;
+    for (;;) {
+      const bool more = w < total;
+      Piece p;
+      p.n_steps = 0;
+      long long next = 0;
+      if (more) {
+        if (lane == 0) next = (long long)atomicAdd(a.sched, 1u) + gridDim.x;
+        if (w < heavy_work) {
+          const int piece = (int)(w / g.Hkv);
+          p.head = (int)(w - (long long)piece * g.Hkv);
+          Heavy x;
+          for (;; ++at_heavy) {
+            const int4* src = reinterpret_cast<const int4*>(heavy + at_heavy);
+            *reinterpret_cast<int4*>(&x) = __ldcg(src);
+            *(reinterpret_cast<int4*>(&x) + 1) = __ldcg(src + 1);
+            if (piece < x.first_piece + x.n_chunks) break;
+          }
+          int b0, bn, bkv;
+          lengths(a, x.seq, b0, bn, bkv);
+          const int h = p.head;
+          tile_piece(a, x.seq, b0, bn, bkv, x.t, p);
+          p.head = h;
+          const int c = piece - x.first_piece, rows = p.n_tok * g.G;
+          p.step0 = c * x.chunk_steps;
+          p.n_steps = min(x.chunk_steps, p.n_steps - p.step0);
+          if (x.n_chunks > 1) {
+            p.n_chunks = x.n_chunks;
+            p.chunk_steps = x.chunk_steps;
+            p.part_step = g.Hkv * rows;
+            p.part_row = x.part_row + c * p.part_step + h * rows;
+            p.counter = x.counter + 2 * h;
+          }
+        } else {
+          const int e = (int)((w - heavy_work) / g.Hkv);
+          p.head = (int)(w - heavy_work - (long long)e * g.Hkv);
+          while (e >= strip_first + strip_all) {
+            strip += 32;
+            strip_first += strip_all;
+            nt = 0;
+            if (strip + lane < a.n_seqs) {
+              lengths(a, strip + lane, s0, n, kv);
+              nt = (n + size - 1) / size;
+            }
+            incl = nt;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int v = __shfl_up_sync(0xffffffffu, incl, o);
+              if (lane >= o) incl += v;
+            }
+            strip_all = __shfl_sync(0xffffffffu, incl, 31);
+          }
+          const int own = __popc(__ballot_sync(0xffffffffu, strip_first + incl <= e));
+          const int h = p.head, t = e - strip_first - __shfl_sync(0xffffffffu, incl - nt, own);
+          tile_piece(a, strip + own, __shfl_sync(0xffffffffu, s0, own), __shfl_sync(0xffffffffu, n, own), __shfl_sync(0xffffffffu, kv, own), t, p);
+          p.head = h;
+          if (is_heavy(p.n_steps, all_steps)) {     // it was among those
+            w = __shfl_sync(0xffffffffu, next, 0);
+            continue;
+          }
+        }
+        if (a.partial) {
+          const bool whole = p.n_chunks == 1;
+          if (p.head == 0 && p.step0 == 0)
+            for (int i = lane; i < p.n_tok; i += 32)
+              a.token_parts[p.tok0 + i] = whole ? PagedToken{(p.tok0 + i) * g.Hq, 1, 0, g.G}
+                                                : PagedToken{p.part_row + i * g.G, p.n_chunks, p.part_step, p.n_tok * g.G};
+        }
+      }
+      const int i = n_given & 1;
+      if (!__all_sync(0xffffffffu, mbar_wait_far(&ctl, piece_empty(i), ((n_given >> 1) & 1u) ^ 1u, 0x900u))) break;
+      if (lane == 0) {
+        tail.piece[i] = p;
+        mbar_arrive(piece_full(i));
+      }
+      __syncwarp();
+      ++n_given;
+      if (!more) {
+        // the last CTA that finds nothing leaves the counter ready for the next launch
+        if (lane == 0 && atomicAdd(a.sched + 1, 1u) == gridDim.x - 1) { a.sched[0] = 0u; a.sched[1] = 0u; }
+        break;
+      }
+      w = __shfl_sync(0xffffffffu, next, 0);
+    }
+  } else if (warp == kProducerWarp) {
     // ------------------------------------------------------------ K and V, a copy per page box and half of the columns
     if (lane == 0) { tma_prefetch_desc(&k_map); tma_prefetch_desc(&v_map); }
     const int copies = 2 * (kTileKeys >> a.lg_box);
@@ -319,14 +434,13 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     int slot = 0;
     uint32_t ph = 1;                         // parity of a slot's emptiness
     bool ok = true;
-    Deal deal(n_work);
-    for (int w; ok && (w = deal.next()) >= 0;) {
-      const int e = w / g.Hkv, h = w - e * g.Hkv;
-      const PagedItem it = load_item(a.items, e);
+    Piece it;
+    while (ok && take_piece(it)) {
+      const int h = it.head;
       const int* table = a.block_table + (size_t)it.seq * g.max_pages;
       int ids = 0, ids_at = -1;
-      for (int j = it.step0; ok && j < it.step0 + it.n_steps; ++j) {
-        const int row0 = (j < it.near_tiles ? j : j + it.skip) * kTileKeys;
+      for (int j = 0; ok && j < it.n_steps; ++j) {
+        const int row0 = step_row(it, j);
         const int pg = row0 >> g.lg_page, pg_last = (row0 + kTileKeys - 1) >> g.lg_page;
         if (ids_at < 0 || pg < ids_at || pg_last >= ids_at + 32) {
           ids_at = pg;
@@ -355,25 +469,48 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       }
     }
   } else if (warp == kQWarp) {
-    // ------------------------------------------------------------ the query blocks of the streams
-    if (lane == 0) {
-      tma_prefetch_desc(&q_map);
-      uint32_t ph[2] = {1u, 1u};
-      bool ok = true;
-      Deal deal(n_work);
-      for (int w; ok && (w = deal.next()) >= 0;) {
-        const int e = w / g.Hkv, h = w - e * g.Hkv;
-        const PagedItem it = load_item(a.items, e);
+    // ------------------------------------------------------------ the query blocks of the streams; unseen rows of V
+    if (lane == 0) tma_prefetch_desc(&q_map);
+    uint32_t ph[2] = {1u, 1u}, rph = 0;
+    int slot = 0;                            // the ring holds K and V in turn
+    bool ok = true;
+    Piece it;
+    while (ok && take_piece(it)) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (s * R >= it.n_tok) break;
-          ok = ok && mbar_wait_far(&ctl, q_empty(s), ph[s], 0x200u);
-          if (!ok) break;
-          ph[s] ^= 1u;
+      for (int s = 0; s < 2; ++s) {
+        if (s * R >= it.n_tok) break;
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, q_empty(s), ph[s], 0x200u));
+        if (!ok) break;
+        ph[s] ^= 1u;
+        if (lane == 0) {
           mbar_arrive_expect_tx(q_full(s), 2u * (uint32_t)(R * g.G) * kLineBytes);
           for (int half = 0; half < 2; ++half)
-            tma_load_4d(q_base + s * kTileBytes + half * (kTileBytes / 2), &q_map, q_full(s), half * kHalfCols, 0, h, it.tok0 + s * R);
+            tma_load_4d(q_base + s * kTileBytes + half * (kTileBytes / 2), &q_map, q_full(s), half * kHalfCols, 0, it.head, it.tok0 + s * R);
         }
+        __syncwarp();
+      }
+      // Rows of V that none of the tokens sees may hold anything (or have not been loaded), and zero times that could be a NaN: they
+      // become zeros before the product.  (Done by the issuing warp, a tile of a window's border or a prompt's end cost it 2500 cycles.)
+      // Every tile of the ring passes here, so that this warp is never a round of the ring behind or ahead of it.
+      for (int f = 0; ok && f < 2 * it.n_steps; ++f) {
+        ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, full(slot), rph, 0x280u));
+        if (!ok) break;
+        const int row0 = step_row(it, f >> 1);
+        if ((f & 1) && unseen_rows(it, row0)) {
+          unsigned char* const mine = smem_al + (2 + slot) * kTileBytes + ((lane >> 3) & 1) * (kTileBytes / 2) + (lane & 7) * 16;
+          auto clear = [&](int r0, int r1) {
+#pragma unroll 4
+            for (int r = max(r0, 0) + (lane >> 4); r < min(r1, kTileKeys); r += 2)
+              *reinterpret_cast<uint4*>(mine + r * kLineBytes) = make_uint4(0u, 0u, 0u, 0u);
+          };
+          clear(it.kv_end - row0, kTileKeys);
+          clear(g.n_sink - row0, min(it.win_lo, it.kv_end) - row0);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(clean(slot));
+        }
+        if (lane == 0) mbar_arrive(empty(slot));
+        if (++slot == kSlots) { slot = 0; rph ^= 1u; }
       }
     }
   } else if (warp == kMmaWarp) {
@@ -426,9 +563,9 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       if (leader) umma_commit(bar);
       __syncwarp();
     };
-    Deal deal(n_work);
-    for (int w; ok && (w = deal.next()) >= 0;) {
-      const PagedItem it = load_item(a.items, w / g.Hkv);
+    uint32_t cleaned = 0;                   // parity of each slot's barrier
+    Piece it;
+    while (ok && take_piece(it)) {
       const bool dual = it.n_tok > R;
       const int n = it.n_steps;
       int ks, vs;
@@ -447,18 +584,10 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       for (int j = 0; j < n; ++j) {
         take(vs);
         if (!ok) break;
-        // rows of V that none of the tokens sees may hold anything (or have not been loaded), and zero times that could be
-        // a NaN: they become zeros
-        const int row0 = (it.step0 + j < it.near_tiles ? it.step0 + j : it.step0 + j + it.skip) * kTileKeys;
-        if (row0 + kTileKeys > it.kv_end || (row0 < it.win_lo && row0 + kTileKeys > g.n_sink)) {
-          unsigned char* const vt = smem_al + 2 * kTileBytes + vs * kTileBytes;
-          for (int r = lane >> 4; r < kTileKeys; r += 2) {
-            const int t = row0 + r;
-            if (t >= it.kv_end || (t < it.win_lo && t >= g.n_sink))
-              *reinterpret_cast<uint4*>(vt + ((lane >> 3) & 1) * (kTileBytes / 2) + r * kLineBytes + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
+        if (unseen_rows(it, step_row(it, j))) {
+          ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, clean(vs), (cleaned >> vs) & 1u, 0x380u));
+          cleaned ^= 1u << vs;
+          if (!ok) break;
         }
         const bool more = j + 1 < n;
         for (int s = 0; s < 2; ++s) {
@@ -501,13 +630,26 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     volatile float* const my_max = &tail.max[s][half][r];
     const volatile float* const other_max = &tail.max[s][half ^ 1][r];
     auto meet = [&]() { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + s) : "memory"); };   // the stream's two warpgroups
+    auto any_of_stream = [&](bool x) {
+      uint32_t r;
+      asm volatile(
+          "{\n"
+          ".reg .pred p, q;\n"
+          "setp.ne.u32 p, %1, 0;\n"
+          "barrier.cta.red.or.pred q, %2, 256, p;\n"
+          "selp.u32 %0, 1, 0, q;\n"
+          "}\n"
+          : "=r"(r) : "r"((uint32_t)x), "r"(1 + s) : "memory");
+      return r != 0;
+    };
     uint32_t sph = 0, oph = 0;
-    bool ok = true;
-    Deal deal(n_work);
-    for (int w; ok && (w = deal.next()) >= 0;) {
-      const int e = w / g.Hkv, h = w - e * g.Hkv;
-      const PagedItem it = load_item(a.items, e);
+    Piece it;
+    // The warps of a stream meet at barriers, so they leave the loop together, and a wait that runs out (after which all others
+    // of the CTA return at once) takes none of them out of a piece.
+    for (;;) {
+      if (any_of_stream(!take_piece(it))) break;
       if (s * R >= it.n_tok) continue;
+      const int h = it.head;
       const int pos = it.pos0 + i_tok;
       const int tok_last = min(it.n_tok, (s + 1) * R) - 1;
       // the keys from clear_lo (or from the first, as far as the sinks go) up to clear_hi are seen by all rows of the stream
@@ -516,10 +658,9 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       float ref = -INFINITY, l = 0.f;       // reference of the row's terms (log2 domain), the sum of this thread's
 #pragma unroll 1
       for (int j = 0; j < it.n_steps; ++j) {
-        const int row0 = (it.step0 + j < it.near_tiles ? it.step0 + j : it.step0 + j + it.skip) * kTileKeys;
-        // (a wait that runs out leaves the loop together with the other warps of the stream, or they would wait at `meet`: both
-        // see the same barrier, and none of the phases behind it will complete)
-        ok = __all_sync(0xffffffffu, mbar_wait(&ctl, s_full(s), sph, 0x600u));
+        const int row0 = step_row(it, j);
+        mbar_wait(&ctl, s_full(s), sph, 0x600u);
+        __syncwarp();
         sph ^= 1u;
         tc_fence_after_sync();
         uint32_t x[2][32];
@@ -535,9 +676,10 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             const int k0 = key0 + 32 * q;
             uint32_t seen = below(min(it.kv_end, pos + 1) - k0);
             if (g.window) seen &= ~below(pos - g.window + 1 - k0) | below(g.n_sink - k0);
+            if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
 #pragma unroll
             for (int c = 0; c < 32; ++c)
-              if (!((seen >> c) & 1u)) x[q][c] = 0xff800000u;
+              if (!(seen & (1u << c))) x[q][c] = 0xff800000u;
           }
         }
         float mx[4];
@@ -587,10 +729,9 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         }
         const float2 t = unpack2(add2(sum0, sum1));
         l += t.x + t.y;
-        if (!ok) break;
       }
-      if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(&ctl, o_full(s), oph, 0x700u));
+      mbar_wait(&ctl, o_full(s), oph, 0x700u);
+      __syncwarp();
       oph ^= 1u;
       tc_fence_after_sync();
       // the row's sum, of the lower keys and the upper ones in this order
@@ -599,43 +740,80 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       const float l_other = *other_max;
       l = half ? l_other + l : l + l_other;
       meet();                                            // (the next item writes there)
-      if (!ok) break;
-      const bool valid = in_block && i_tok < it.n_tok;
-      if (it.part_row < 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;        // no key seen: zeros
-        const size_t row = (size_t)(it.tok0 + i_tok) * g.Hq + h * g.G + head;
-        uint4* const dst = reinterpret_cast<uint4*>(a.out) + row * (kD / 8) + half * 8;
-        const bool store = valid && it.part_row == -1;
+      // O comes out of tensor memory with a row in a quad of lanes, eight columns of each of its groups of 32 bits, and is stored as
+      // it comes (partial rows) or after the lanes of a quad have traded for 16 bytes in a row: a store of a warp then touches eight
+      // rows.  (With a thread to a row each touched 32, and an item's end took 8000 cycles.)
+      const float inv = l == 0.f ? 0.f : 1.f / l;        // no key seen: zeros
+      const bool last_chunk = it.n_chunks > 1;
+      const bool final = !a.partial && !last_chunk;
+      const size_t head_row = (size_t)it.tok0 * g.Hq + h * g.G;     // output row of the item's first token and the group's first head
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {                      // 16 rows each
+        uint32_t o[32];
+        tmem_ld_16x64(o_addr + ((uint32_t)(16 * e) << 16), o);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t o[32];
-          tmem_ld32(o_addr + 32 * q, o);
-          if (store) {
+        for (int u = 0; u < 2; ++u) {                    // the upper and the lower eight of them
+          const int in_warp = 16 * e + 8 * u + (lane >> 2);
+          const int row = (warp & 3) * 32 + in_warp;
+          const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
+          const bool valid = row < R * g.G && i < it.n_tok;
+          if (final) {
+            const float f = __shfl_sync(0xffffffffu, inv, in_warp);
+            uint4* const dst = reinterpret_cast<uint4*>(a.out) + (head_row + (size_t)i * g.Hq + hd) * (kD / 8) + half * 8 + (lane & 3);
 #pragma unroll
-            for (int c = 0; c < 32; c += 8) {
-              uint4 v;
-              v.x = pack16<kF16>(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv);
-              v.y = pack16<kF16>(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
-              v.z = pack16<kF16>(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv);
-              v.w = pack16<kF16>(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv);
-              dst[q * 4 + c / 8] = v;
+            for (int b = 0; b < 2; ++b) {                // 32 columns each
+              uint32_t v[4];
+#pragma unroll
+              for (int c = 0; c < 4; ++c)
+                v[c] = pack16<kF16>(__uint_as_float(o[16 * b + 4 * c + 2 * u]) * f, __uint_as_float(o[16 * b + 4 * c + 2 * u + 1]) * f);
+              const uint4 t = quad_transpose(v, lane);
+              if (valid) dst[4 * b] = t;
+            }
+          } else {
+            const size_t to = last_chunk ? (size_t)it.part_row + (size_t)i * g.G + hd : head_row + (size_t)i * g.Hq + hd;
+            float* const dst = a.parts + to * kPagedPartStride + half * 64 + 2 * (lane & 3);
+            if (valid && (long long)to < a.max_rows) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c)
+                __stcg(reinterpret_cast<float2*>(dst + 8 * c), make_float2(__uint_as_float(o[4 * c + 2 * u]), __uint_as_float(o[4 * c + 2 * u + 1])));
             }
           }
         }
-        if (store && a.lse && half == 0) a.lse[row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
-      } else {
-        float* const dst = a.parts + ((size_t)it.part_row + (size_t)h * it.rows + (size_t)i_tok * g.G + head) * kPagedPartStride;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t o[32];
-          tmem_ld32(o_addr + 32 * q, o);
-          if (valid) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 4)
-              *reinterpret_cast<uint4*>(dst + half * 64 + 32 * q + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-          }
-        }
-        if (valid && half == 0) *reinterpret_cast<float2*>(dst + kD) = make_float2(ref, l);
+      }
+      const bool valid = in_block && i_tok < it.n_tok && half == 0;
+      if (final) {
+        if (valid && a.lse) a.lse[head_row + (size_t)i_tok * g.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
+        continue;
+      }
+      const size_t to = last_chunk ? (size_t)it.part_row + (size_t)i_tok * g.G + head : head_row + (size_t)i_tok * g.Hq + head;
+      if (valid && (long long)to < a.max_rows) __stcg(reinterpret_cast<float2*>(a.parts + to * kPagedPartStride + kD), make_float2(ref, l));
+      if (a.partial) continue;
+      // the last of the tile's chunks to arrive joins them all
+      __threadfence();
+      meet();
+      if ((tid & 255) == 0) {
+        unsigned* const count = a.sched + 16 + it.counter + s;
+        const bool last = atomicAdd(count, 1u) == (unsigned)(it.n_chunks - 1);
+        if (last) *count = 0u;                           // ready for the next launch
+        __threadfence();
+        tail.last[s] = last;
+      }
+      meet();
+      if (!*reinterpret_cast<volatile int*>(&tail.last[s])) continue;
+      const int n_rows = min(R, it.n_tok - s * R) * g.G, row_at = s * R * g.G;
+      const size_t first_row = (size_t)it.part_row - (size_t)(it.step0 / it.chunk_steps) * it.part_step + row_at;
+      for (int row = warp & 7; row < n_rows; row += 8) {
+        Partial p;
+        p.clear();
+        join_rows(p, it.n_chunks, lane, [&](int c) { return a.parts + (first_row + (size_t)c * it.part_step + row) * kPagedPartStride; });
+        const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
+        const float f = p.l == 0.f ? 0.f : 1.f / p.l;
+        uint2 v;
+        v.x = pack16<kF16>(p.o[0] * f, p.o[1] * f);
+        v.y = pack16<kF16>(p.o[2] * f, p.o[3] * f);
+        const size_t out_row = head_row + (size_t)i * g.Hq + hd;
+        reinterpret_cast<uint2*>(a.out)[out_row * (kD / 4) + lane] = v;
+        if (a.lse && lane == 0) a.lse[out_row] = p.l == 0.f ? -INFINITY : (p.m + log2f(p.l)) * kLn2;
       }
     }
   }
@@ -645,31 +823,6 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 512);
-  }
-}
-
-// Rows of the tiles that were cut along the keys: a warp to a row, four outputs a lane, the chunks in their order.
-template <bool kF16>
-__global__ void __launch_bounds__(256) paged_combine_kernel(const KernelArgs a, const PagedTile* tiles) {
-  pdl_trigger();
-  pdl_wait();
-  const PagedGeom& g = a.g;
-  const int lane = threadIdx.x & 31;
-  const long long n = (long long)a.head->n_split * g.Hkv * kPagedRows;
-  for (long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5; w < n; w += (long long)gridDim.x * (blockDim.x >> 5)) {
-    const int r = (int)(w % kPagedRows), h = (int)((w / kPagedRows) % g.Hkv);
-    const int4 t = __ldg(reinterpret_cast<const int4*>(tiles) + w / kPagedRows / g.Hkv);   // {row, chunks, rows, first token}
-    if (r >= t.z) continue;
-    Partial p;
-    p.o[0] = p.o[1] = p.o[2] = p.o[3] = 0.f; p.m = -INFINITY; p.l = 0.f;
-    join_rows(p, t.y, lane, [&](int i) { return a.parts + ((size_t)t.x + ((size_t)i * g.Hkv + h) * t.z + r) * kPagedPartStride; });
-    const size_t row = (size_t)(t.w + r / g.G) * g.Hq + h * g.G + r % g.G;
-    const float inv = p.l == 0.f ? 0.f : 1.f / p.l;
-    uint2 v;
-    v.x = pack16<kF16>(p.o[0] * inv, p.o[1] * inv);
-    v.y = pack16<kF16>(p.o[2] * inv, p.o[3] * inv);
-    reinterpret_cast<uint2*>(a.out)[row * (kD / 4) + lane] = v;
-    if (a.lse && lane == 0) a.lse[row] = p.l == 0.f ? -INFINITY : (p.m + log2f(p.l)) * kLn2;
   }
 }
 
@@ -685,35 +838,25 @@ cudaError_t launch(const PagedAttnArgs& d, const PagedWs& ws, cudaStream_t st) {
   static OncePerDevice granted;
   cudaError_t e = grant_smem(paged_attention_kernel<kF16>, kSmemBytes, granted);
   if (e != cudaSuccess) return e;
-  PlanArgs p{};
-  p.g = d.g;
-  p.q_start = d.q_start; p.kv_len = d.kv_len;
-  p.n_seqs = d.n_seqs; p.causal = d.causal; p.partial = d.partial; p.grid = kSms;
-  const int tokens = 128 / d.g.G;
-  p.item_tokens = 2 * tokens;
-  p.head = (PagedPlanHeader*)(d.wsp + kPagedPlan);
-  p.items = (PagedItem*)(d.wsp + ws.items);
-  p.tiles = (PagedTile*)(d.wsp + ws.tiles);
-  p.max_tiles = ws.max_tiles; p.max_items = ws.max_items; p.max_split = ws.max_split; p.max_rows = ws.max_rows;
   KernelArgs a{};
   a.g = d.g;
-  a.block_table = d.block_table; a.head = p.head; a.items = p.items;
-  a.parts = (float*)(d.wsp + ws.part_o);
-  a.out = d.out; a.lse = d.lse;
-  a.tokens = tokens;
+  a.block_table = d.block_table; a.q_start = d.q_start; a.kv_len = d.kv_len;
+  a.n_seqs = d.n_seqs; a.causal = d.causal; a.partial = d.partial;
+  a.tokens = 128 / d.g.G;
+  a.g_inv = 65536 / d.g.G + 1;
   a.box_rows = std::min(d.g.page, kTileKeys);
   while ((1 << a.lg_box) < a.box_rows) ++a.lg_box;
+  a.sched = (unsigned*)(d.wsp + ws.sched);
+  a.heavy = (Heavy*)(d.wsp + ws.heavy);
+  a.token_parts = (PagedToken*)(d.wsp + ws.tokens);
+  a.parts = (float*)(d.wsp + ws.part_o);
+  a.max_rows = ws.max_rows;
+  a.out = d.out; a.lse = d.lse;
   CUtensorMap qm, km, vm;
-  if (!paged_q_map(&qm, d.q, d.g, tokens) || !paged_kv_map(&km, d.K, d.g, a.box_rows, 0) || !paged_kv_map(&vm, d.V, d.g, a.box_rows, 0))
+  if (!paged_q_map(&qm, d.q, d.g, a.tokens) || !paged_kv_map(&km, d.K, d.g, a.box_rows, 0) || !paged_kv_map(&vm, d.V, d.g, a.box_rows, 0))
     return cudaErrorInvalidValue;
-  e = launch_pdl(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
-  if (e == cudaSuccess) e = launch_pdl(paged_attention_kernel<kF16>, dim3(kSms), dim3(kThreads), kSmemBytes, st, qm, km, vm, a);
-  if (e != cudaSuccess) return e;
-  count_launch(2);
-  if (!d.partial) {
-    e = launch_pdl(paged_combine_kernel<kF16>, dim3(4 * kSms), dim3(256), 0, st, a, (const PagedTile*)p.tiles);
-    if (e == cudaSuccess) count_launch(1);
-  }
+  e = launch_pdl(paged_attention_kernel<kF16>, dim3(kSms), dim3(kThreads), kSmemBytes, st, qm, km, vm, a);
+  if (e == cudaSuccess) count_launch(1);
   return e;
 }
 
@@ -730,16 +873,14 @@ bool paged_kv_map(CUtensorMap* out, const void* base, const PagedGeom& g, int ro
 
 PagedWs paged_ws(int B, int Hq, int Hkv, int n_tokens, int n_groups) {
   PagedWs w{};
-  const int G = Hq / Hkv, item_tokens = 2 * (128 / G);
-  w.max_tiles = n_tokens / item_tokens + std::max(B, n_groups);
-  w.max_split = kSms;
-  w.max_items = w.max_tiles + kSms;
-  // chunks of cut tiles are no more than the SMs; with a shared prefix every token has a row in any case
-  w.max_rows = (long long)kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)B * Hq : 0);
+  const int G = Hq / Hkv;
+  // chunks of cut tiles are no more than the SMs; with a shared prefix every token has rows of its own in any case
+  w.max_rows = (long long)kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)n_tokens * Hq : 0);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  size_t off = kPagedPlan + 256;
-  w.items = off;  off = up(off + (size_t)w.max_items * sizeof(PagedItem));
-  w.tiles = off;  off = up(off + (size_t)std::max(w.max_split, n_groups ? B : 0) * sizeof(PagedTile));
+  size_t off = kPagedPlan;
+  w.sched = off;  off = up(off + (16 + 2 * kSms) * 4);
+  w.heavy = off;  off = up(off + (size_t)kSms * kMaxHeavy * sizeof(Heavy));
+  w.tokens = off; off = up(off + (size_t)(n_groups ? B : 0) * sizeof(PagedToken));
   w.part_o = off; off = up(off + (size_t)w.max_rows * kPagedPartStride * 4);
   w.total = off;
   return w;
