@@ -135,12 +135,12 @@ __device__ __forceinline__ bool is_heavy(int n, unsigned long long all) { return
 // Into how many chunks a tile of n steps is cut, `all` being the steps of all tiles and heads.  Twice the mean share of an SM or more is cut into as many
 // pieces as it has shares, so that all pieces of cut tiles together are no more than the SMs.  Joining k chunks of `rows` rows costs the
 // last CTA about 8 cycles a row and chunk, and a chunk less takes n / k steps of 3000 cycles off: beyond sqrt(375 n / rows) chunks
-// the joining costs more than it gives (a shared prefix is joined elsewhere, by many).
+// the joining costs more than it gives, and so it does for chunks of less than 8 steps (a shared prefix is joined elsewhere, by many).
 __device__ __forceinline__ int chunks_of(const KernelArgs& a, int n, int rows, unsigned long long all) {
   const unsigned long long shares = (unsigned long long)n * gridDim.x / all;
   if (shares < 2) return 1;
   int k = (int)min(shares, (unsigned long long)n);
-  if (!a.partial) k = max(1, min(k, (int)sqrtf(375.f * n / rows)));
+  if (!a.partial) k = max(1, min(min(k, n / 8), (int)sqrtf(375.f * n / rows)));
   const int len = (n + k - 1) / k;
   return (n + len - 1) / len;
 }
@@ -248,10 +248,12 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     tile_piece(a, lo, s0, n, kv, e - tb[lo], p);
   };
   unsigned long long steps = 0;
+  int my_steps = 0;             // of tile tid
   for (int e = tid; e < n_tiles; e += kThreads) {
     Piece p;
     tile_of(e, p);
     steps += (unsigned)p.n_steps;
+    if (e == tid) my_steps = p.n_steps;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
@@ -267,11 +269,14 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   int n_heavy = 0;
   for (int base = 0; base < n_tiles; base += kThreads) {
     const int e = base + tid;
-    Piece p;
     bool is = false;
     if (e < n_tiles) {
-      tile_of(e, p);
-      is = is_heavy(p.n_steps, all_steps);
+      if (base) {
+        Piece p;
+        tile_of(e, p);
+        my_steps = p.n_steps;
+      }
+      is = is_heavy(my_steps, all_steps);
     }
     if (!__syncthreads_or(is)) continue;
     const unsigned m = __ballot_sync(0xffffffffu, is);
@@ -643,13 +648,20 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       return r != 0;
     };
     uint32_t sph = 0, oph = 0;
-    Piece it;
     // The warps of a stream meet at barriers, so they leave the loop together, and a wait that runs out (after which all others
     // of the CTA return at once) takes none of them out of a piece.
     for (;;) {
-      if (any_of_stream(!take_piece(it))) break;
-      if (s * R >= it.n_tok) continue;
-      const int h = it.head;
+      const int slot = n_taken & 1;
+      const bool there = mbar_wait_far(&ctl, piece_full(slot), (n_taken >> 1) & 1u, 0x800u);
+      const Piece& it = tail.piece[slot];              // read where it lies, and given back at the end
+      const int n_steps = there ? it.n_steps : 0;
+      if (any_of_stream(n_steps == 0)) break;
+      ++n_taken;
+      auto give_back = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(piece_empty(slot));
+      };
+      if (s * R >= it.n_tok) { give_back(); continue; }
       const int pos = it.pos0 + i_tok;
       const int tok_last = min(it.n_tok, (s + 1) * R) - 1;
       // the keys from clear_lo (or from the first, as far as the sinks go) up to clear_hi are seen by all rows of the stream
@@ -657,31 +669,37 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       const int clear_lo = g.window ? it.pos0 + tok_last - g.window + 1 : 0;
       float ref = -INFINITY, l = 0.f;       // reference of the row's terms (log2 domain), the sum of this thread's
 #pragma unroll 1
-      for (int j = 0; j < it.n_steps; ++j) {
+      for (int j = 0; j < n_steps; ++j) {
         const int row0 = step_row(it, j);
         mbar_wait(&ctl, s_full(s), sph, 0x600u);
         __syncwarp();
         sph ^= 1u;
         tc_fence_after_sync();
+        if (row0 + kTileKeys > clear_hi || (row0 < clear_lo && row0 + kTileKeys > g.n_sink)) {
+          // keys that the row does not see become -inf where they lie, 16 columns at a time: in the registers, all unrolled, it was
+          // code of 4 KB that few tiles need, and took 1500 cycles of each
+          const int key0 = row0 + half * 64, hi = min(it.kv_end, pos + 1), lo = pos - g.window + 1;
+          auto below = [](int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1u; };   // the n lowest bits
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            const int k0 = key0 + 16 * q;
+            uint32_t seen = below(hi - k0);
+            if (g.window) seen &= ~below(lo - k0) | below(g.n_sink - k0);
+            if (__all_sync(0xffffffffu, seen == 0xffffu)) continue;
+            uint32_t y[16];
+            tmem_ld16(s_addr + 16 * q, y);
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (!(seen & (1u << c))) y[c] = 0xff800000u;
+            tmem_st16(s_addr + 16 * q, y);
+          }
+          tmem_st_wait();
+        }
         uint32_t x[2][32];
         tmem_ld32_issue(s_addr, x[0]);
         tmem_ld32_issue(s_addr + 32, x[1]);
         tmem_ld_wait(x[0]);
         tmem_ld_wait(x[1]);
-        if (row0 + kTileKeys > clear_hi || (row0 < clear_lo && row0 + kTileKeys > g.n_sink)) {
-          const int key0 = row0 + half * 64;
-          auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // the n lowest bits
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int k0 = key0 + 32 * q;
-            uint32_t seen = below(min(it.kv_end, pos + 1) - k0);
-            if (g.window) seen &= ~below(pos - g.window + 1 - k0) | below(g.n_sink - k0);
-            if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (!(seen & (1u << c))) x[q][c] = 0xff800000u;
-          }
-        }
         float mx[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -744,9 +762,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       // it comes (partial rows) or after the lanes of a quad have traded for 16 bytes in a row: a store of a warp then touches eight
       // rows.  (With a thread to a row each touched 32, and an item's end took 8000 cycles.)
       const float inv = l == 0.f ? 0.f : 1.f / l;        // no key seen: zeros
-      const bool last_chunk = it.n_chunks > 1;
-      const bool final = !a.partial && !last_chunk;
-      const size_t head_row = (size_t)it.tok0 * g.Hq + h * g.G;     // output row of the item's first token and the group's first head
+      const bool cut = it.n_chunks > 1, final = !a.partial && !cut;
+      const int n_tok = it.n_tok;
+      const size_t head_row = (size_t)it.tok0 * g.Hq + it.head * g.G;     // output row of the first token and the group's first head
+      const size_t part_at = cut ? (size_t)it.part_row : head_row;         // and its partial row
+      const int tok_step = cut ? g.G : g.Hq;                               // (of partial rows, from a token to the next)
 #pragma unroll 1
       for (int e = 0; e < 2; ++e) {                      // 16 rows each
         uint32_t o[32];
@@ -756,10 +776,10 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const int in_warp = 16 * e + 8 * u + (lane >> 2);
           const int row = (warp & 3) * 32 + in_warp;
           const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
-          const bool valid = row < R * g.G && i < it.n_tok;
+          const bool valid = row < R * g.G && i < n_tok;
           if (final) {
             const float f = __shfl_sync(0xffffffffu, inv, in_warp);
-            uint4* const dst = reinterpret_cast<uint4*>(a.out) + (head_row + (size_t)i * g.Hq + hd) * (kD / 8) + half * 8 + (lane & 3);
+            uint4* const dst = reinterpret_cast<uint4*>(a.out) + (head_row + (uint32_t)(i * g.Hq + hd)) * (kD / 8) + half * 8 + (lane & 3);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {                // 32 columns each
               uint32_t v[4];
@@ -770,7 +790,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               if (valid) dst[4 * b] = t;
             }
           } else {
-            const size_t to = last_chunk ? (size_t)it.part_row + (size_t)i * g.G + hd : head_row + (size_t)i * g.Hq + hd;
+            const size_t to = part_at + (uint32_t)(i * tok_step + hd);
             float* const dst = a.parts + to * kPagedPartStride + half * 64 + 2 * (lane & 3);
             if (valid && (long long)to < a.max_rows) {
 #pragma unroll
@@ -780,14 +800,15 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           }
         }
       }
-      const bool valid = in_block && i_tok < it.n_tok && half == 0;
-      if (final) {
-        if (valid && a.lse) a.lse[head_row + (size_t)i_tok * g.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
-        continue;
+      if (in_block && i_tok < n_tok && half == 0) {
+        if (final) {
+          if (a.lse) a.lse[head_row + (uint32_t)(i_tok * g.Hq + head)] = l == 0.f ? -INFINITY : (ref + __log2f(l)) * kLn2;
+        } else {
+          const size_t to = part_at + (uint32_t)(i_tok * tok_step + head);
+          if ((long long)to < a.max_rows) __stcg(reinterpret_cast<float2*>(a.parts + to * kPagedPartStride + kD), make_float2(ref, l));
+        }
       }
-      const size_t to = last_chunk ? (size_t)it.part_row + (size_t)i_tok * g.G + head : head_row + (size_t)i_tok * g.Hq + head;
-      if (valid && (long long)to < a.max_rows) __stcg(reinterpret_cast<float2*>(a.parts + to * kPagedPartStride + kD), make_float2(ref, l));
-      if (a.partial) continue;
+      if (final || a.partial) { give_back(); continue; }
       // the last of the tile's chunks to arrive joins them all
       __threadfence();
       meet();
@@ -799,22 +820,43 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         tail.last[s] = last;
       }
       meet();
-      if (!*reinterpret_cast<volatile int*>(&tail.last[s])) continue;
-      const int n_rows = min(R, it.n_tok - s * R) * g.G, row_at = s * R * g.G;
-      const size_t first_row = (size_t)it.part_row - (size_t)(it.step0 / it.chunk_steps) * it.part_step + row_at;
-      for (int row = warp & 7; row < n_rows; row += 8) {
-        Partial p;
-        p.clear();
-        join_rows(p, it.n_chunks, lane, [&](int c) { return a.parts + (first_row + (size_t)c * it.part_step + row) * kPagedPartStride; });
-        const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
-        const float f = p.l == 0.f ? 0.f : 1.f / p.l;
-        uint2 v;
-        v.x = pack16<kF16>(p.o[0] * f, p.o[1] * f);
-        v.y = pack16<kF16>(p.o[2] * f, p.o[3] * f);
-        const size_t out_row = head_row + (size_t)i * g.Hq + hd;
-        reinterpret_cast<uint2*>(a.out)[out_row * (kD / 4) + lane] = v;
-        if (a.lse && lane == 0) a.lse[out_row] = p.l == 0.f ? -INFINITY : (p.m + log2f(p.l)) * kLn2;
+      if (*reinterpret_cast<volatile int*>(&tail.last[s])) {
+        const int n_rows = min(R, n_tok - s * R) * g.G, n_chunks = it.n_chunks, step = it.part_step;
+        const size_t first_row = part_at - (size_t)(it.step0 / it.chunk_steps) * step + s * R * g.G;
+        constexpr int kRows = 4;                         // of a warp at a time, so that their loads are in flight together
+        for (int r0 = warp & 7; r0 < n_rows; r0 += 8 * kRows) {
+          Partial p[kRows];
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) p[k].clear();
+          const float* src = a.parts + (first_row + r0) * kPagedPartStride;
+          for (int c = 0; c < n_chunks; ++c, src += (size_t)step * kPagedPartStride) {
+            float4 o[kRows];
+            float2 ml[kRows];
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) {
+              const float* x = src + (r0 + 8 * k < n_rows ? 8 * k : 0) * kPagedPartStride;
+              o[k] = __ldcg(reinterpret_cast<const float4*>(x) + lane);
+              ml[k] = __ldcg(reinterpret_cast<const float2*>(x + kD));
+            }
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) p[k].join(ml[k].x, ml[k].y, o[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < kRows; ++k) {
+            const int row = r0 + 8 * k;
+            if (row >= n_rows) break;
+            const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
+            const float f = p[k].l == 0.f ? 0.f : 1.f / p[k].l;
+            uint2 v;
+            v.x = pack16<kF16>(p[k].o[0] * f, p[k].o[1] * f);
+            v.y = pack16<kF16>(p[k].o[2] * f, p[k].o[3] * f);
+            const size_t out_row = head_row + (uint32_t)(i * g.Hq + hd);
+            reinterpret_cast<uint2*>(a.out)[out_row * (kD / 4) + lane] = v;
+            if (a.lse && lane == 0) a.lse[out_row] = p[k].l == 0.f ? -INFINITY : (p[k].m + __log2f(p[k].l)) * kLn2;
+          }
+        }
       }
+      give_back();
     }
   }
   tc_fence_before_sync();
