@@ -18,8 +18,6 @@
 //   * S(j+1) may be issued behind P V(j), which reads P from the same columns;
 //   * a stream that has been told of S(j) also knows that its P V(j-1) is done, and may rescale O itself.
 // P is handed over in two halves, so that P V begins while the second is worked on.
-// O is rescaled only when a row's maximum has grown by more than 2^8 over its reference, which on real logits is a few times a
-// row; until then terms are at most 2^8, and the sums and O hold that in 32 bits.
 #include <algorithm>
 
 #include "exp2.cuh"
@@ -623,8 +621,10 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     }
   } else if (warp < kSoftmaxWarps) {
     // ------------------------------------------------------------ softmax: two threads to a row
-    constexpr float kBias = kF16 ? 7.f : 0.f;     // (see pack16; with the 2^8 of the lazy rescaling below the largest fp16)
-    constexpr float kLazy = 8.f;
+    // O is rescaled when a row's maximum has grown by more than 2^kLazy over its reference.  In bf16 as in fp32 a factor costs no
+    // bits, so that is where terms and sums are still far from the largest numbers, and hardly ever happens; in fp16 terms have to
+    // stay below 2^16 (and are kept 2^kBias higher than they are, see pack16).
+    constexpr float kBias = kF16 ? 7.f : 0.f, kLazy = kF16 ? 8.f : 40.f;
     const int s = warp >> 3, half = (warp >> 2) & 1, r = tid & 127;
     const uint32_t lane_bits = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem_base + lane_bits + (uint32_t)(s * 128 + half * 64), o_addr = s_addr + kColO;
@@ -646,6 +646,26 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           "}\n"
           : "=r"(r) : "r"((uint32_t)x), "r"(1 + s) : "memory");
       return r != 0;
+    };
+    auto max_of = [](const uint32_t (&x)[32]) {
+      float m[2] = {__uint_as_float(x[0]), __uint_as_float(x[1])};
+#pragma unroll
+      for (int c = 2; c < 30; c += 4) {
+        m[0] = max3(m[0], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+        m[1] = max3(m[1], __uint_as_float(x[c + 2]), __uint_as_float(x[c + 3]));
+      }
+      return max3(fmaxf(m[0], m[1]), __uint_as_float(x[30]), __uint_as_float(x[31]));
+    };
+    // exp2(scale2 x - ref) of 32 keys, rounded in pairs, and their sum
+    auto terms = [&](const uint32_t (&x)[32], float ref, uint32_t (&packed)[16], f32x2& sum) {
+      const f32x2 nref = pack2(ref == -INFINITY ? 0.f : -ref);
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        const f32x2 y = exp2_pair<false>(fma2(pack2(x[c], x[c + 1]), sc, nref), c / 2);
+        sum = add2(sum, y);
+        const float2 p = unpack2(y);
+        packed[c >> 1] = pack16<kF16>(p.x, p.y);
+      }
     };
     uint32_t sph = 0, oph = 0;
     // The warps of a stream meet at barriers, so they leave the loop together, and a wait that runs out (after which all others
@@ -695,57 +715,44 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           }
           tmem_st_wait();
         }
-        uint32_t x[2][32];
-        tmem_ld32_issue(s_addr, x[0]);
-        tmem_ld32_issue(s_addr + 32, x[1]);
-        tmem_ld_wait(x[0]);
-        tmem_ld_wait(x[1]);
-        float mx[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          mx[q] = __uint_as_float(x[q >> 1][(q & 1) * 16]);
-#pragma unroll
-          for (int c = 1; c < 16; ++c) mx[q] = fmaxf(mx[q], __uint_as_float(x[q >> 1][(q & 1) * 16 + c]));
-        }
-        float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        *my_max = top;
-        meet();
-        top = fmaxf(top, *other_max) * g.scale2 - kBias;
-        const bool grow = top > ref + kLazy;             // (from -inf on the first key that is seen)
-        if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? ex2_approx(ref - top) : 1.f;
+        // (The upper 32 keys are read twice, first for their maximum alone: with 64 logits held, a thread's 96 registers leave no room
+        // for more than a few exponentials at a time, and these took 700 cycles instead of the unit's 420 for 32 keys.)
+        uint32_t x[32], packed[16];
+        tmem_ld32(s_addr + 32, x);
+        float top = max_of(x);
+        tmem_ld32(s_addr, x);
+        top = fmaxf(top, max_of(x));
+        if (any_of_stream(top * g.scale2 - kBias > ref + kLazy)) {       // (from -inf on the first key that is seen)
+          *my_max = top;
+          meet();
+          const float t = fmaxf(top, *other_max) * g.scale2 - kBias;
+          const bool grow = t > ref + kLazy;
+          const float f = grow ? ex2_approx(ref - t) : 1.f;
           const bool had = __any_sync(0xffffffffu, grow && ref > -INFINITY);
-          if (grow) { l *= f; ref = top; }
+          if (grow) { l *= f; ref = t; }
           if (had && j > 0) {                            // this half of O's columns
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
-              uint32_t o[16];
-              tmem_ld16(o_addr + 16 * q, o);
+              tmem_ld16(o_addr + 16 * q, packed);
 #pragma unroll
-              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-              tmem_st16(o_addr + 16 * q, o);
+              for (int c = 0; c < 16; ++c) packed[c] = __float_as_uint(__uint_as_float(packed[c]) * f);
+              tmem_st16(o_addr + 16 * q, packed);
             }
           }
         }
-        const f32x2 nref = pack2(ref == -INFINITY ? 0.f : -ref);
-        f32x2 sum0 = 0ull, sum1 = 0ull;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t packed[16];
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const f32x2 y = exp2_pair<false>(fma2(pack2(x[q][c], x[q][c + 1]), sc, nref), c / 2);
-            if (c & 2) sum1 = add2(sum1, y);
-            else sum0 = add2(sum0, y);
-            const float2 p = unpack2(y);
-            packed[c >> 1] = pack16<kF16>(p.x, p.y);
-          }
-          tmem_st16(s_addr + 16 * q, packed);
-          tmem_st_wait();
-          tc_fence_before_sync();
-          mbar_arrive(p_full(s, q));
-        }
-        const float2 t = unpack2(add2(sum0, sum1));
+        f32x2 sum = 0ull;
+        terms(x, ref, packed, sum);
+        tmem_st16(s_addr, packed);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        mbar_arrive(p_full(s, 0));
+        tmem_ld32(s_addr + 32, x);
+        terms(x, ref, packed, sum);
+        tmem_st16(s_addr + 16, packed);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        mbar_arrive(p_full(s, 1));
+        const float2 t = unpack2(sum);
         l += t.x + t.y;
       }
       mbar_wait(&ctl, o_full(s), oph, 0x700u);
