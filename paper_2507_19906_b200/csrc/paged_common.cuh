@@ -68,6 +68,13 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 
+// The first eight of 16 values to as many columns of this thread's lane.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 // 64 fp32 columns of 16 lanes of tensor memory, a lane's columns spread over four threads: thread t has of lane t / 4 (and t / 4 + 8)
 // columns 8 c + 2 (t % 4) and the next one in r[4 c], r[4 c + 1] (and r[4 c + 2], r[4 c + 3]), c = 0..7.
 __device__ __forceinline__ void tmem_ld_16x64(uint32_t taddr, uint32_t (&r)[32]) {

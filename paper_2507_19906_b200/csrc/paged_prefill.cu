@@ -13,11 +13,11 @@
 //
 // A CTA works on two streams of 128 rows; while one stream has its softmax the other has the tensor cores.  A stream is two
 // warpgroups, two threads to a row, 64 of a tile's keys each.  Tensor memory: S of the streams at columns 0 and 128, O at 256 and
-// 384.  P, rounded to 16 bits, overwrites S, the first 32 of the 64 columns of each warpgroup.  One warp issues all MMAs, and those of
-// an issuing thread run in order, so
+// 384.  P, rounded to 16 bits, overwrites S, the first 32 of the 64 columns of each warpgroup.  One warp issues all MMAs of a stream, and
+// those of an issuing thread run in order, so
 //   * S(j+1) may be issued behind P V(j), which reads P from the same columns;
 //   * a stream that has been told of S(j) also knows that its P V(j-1) is done, and may rescale O itself.
-// P is handed over in two halves, so that P V begins while the second is worked on.
+// P is handed over in two parts, of 48 keys and 16, so that little of P V is left when the last is done.
 #include <algorithm>
 
 #include "exp2.cuh"
@@ -32,13 +32,13 @@ namespace {
 using namespace tc;
 
 constexpr int kSoftmaxWarps = 16;                 // two streams of two warpgroups
-constexpr int kProducerWarp = 16, kMmaWarp = 17, kQWarp = 18, kSchedWarp = 19;
+constexpr int kProducerWarp = 16, kStewardWarp = 17, kMmaWarp = 18;
 constexpr int kThreads = 640;
 constexpr int kSlots = 5;                         // K and V tiles in one ring, in the order in which they are used
 constexpr int kTileBytes = kKvTileBytes;          // 32 KB
 constexpr uint32_t kColO = 256;
 constexpr int kMaxHeavy = 2 * kSms;               // tiles of at least half an SM's mean share
-constexpr int kItemReaders = kSoftmaxWarps + 3;   // warps that take a piece from the scheduler
+constexpr int kItemReaders = kSoftmaxWarps + 2;   // warps that take a piece from the producer
 
 // A piece of work: a tile of rows of one kv head against a range of steps.
 struct Piece {
@@ -69,7 +69,7 @@ struct Heavy {
 
 // What is in shared memory beside the two query blocks and the ring.
 struct Tail {
-  unsigned long long bars[3 * kSlots + 16];
+  unsigned long long bars[2 * kSlots + 14];
   Piece piece[2];
   float max[2][2][128];                           // [stream][half][row]: maxima of a tile's halves, and at the end the sums
   uint32_t tmem;
@@ -143,6 +143,19 @@ __device__ __forceinline__ int chunks_of(const KernelArgs& a, int n, int rows, u
   return (n + len - 1) / len;
 }
 
+// exp2(scale2 x - ref) of keys kFrom..kTo - 1, rounded in pairs, and their sum
+template <bool kF16, int kFrom, int kTo>
+__device__ __forceinline__ void terms(const uint32_t (&x)[32], f32x2 scale2, float ref, uint32_t (&packed)[16], f32x2& sum) {
+  const f32x2 nref = pack2(ref == -INFINITY ? 0.f : -ref);
+#pragma unroll
+  for (int c = kFrom; c < kTo; c += 2) {
+    const f32x2 y = exp2_pair<false>(fma2(pack2(x[c], x[c + 1]), scale2, nref), c / 2);
+    sum = add2(sum, y);
+    const float2 p = unpack2(y);
+    packed[(c - kFrom) >> 1] = pack16<kF16>(p.x, p.y);
+  }
+}
+
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -158,21 +171,19 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (kSlots + s); };
   auto q_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };
-  auto q_empty = [&](int s) { return bar0 + 8u * (2 * kSlots + 2 + s); };
-  auto s_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 4 + s); };
-  auto p_full = [&](int s, int part) { return bar0 + 8u * (2 * kSlots + 6 + 2 * part + s); };
-  auto o_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 10 + s); };
-  auto piece_full = [&](int i) { return bar0 + 8u * (2 * kSlots + 12 + i); };
-  auto piece_empty = [&](int i) { return bar0 + 8u * (2 * kSlots + 14 + i); };
-  auto clean = [&](int s) { return bar0 + 8u * (2 * kSlots + 16 + s); };   // the tile of V in the slot has had its unseen rows cleared
+  auto s_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 2 + s); };
+  auto p_full = [&](int s, int part) { return bar0 + 8u * (2 * kSlots + 4 + 2 * part + s); };
+  auto o_full = [&](int s) { return bar0 + 8u * (2 * kSlots + 8 + s); };
+  auto piece_full = [&](int i) { return bar0 + 8u * (2 * kSlots + 10 + i); };
+  auto piece_empty = [&](int i) { return bar0 + 8u * (2 * kSlots + 12 + i); };
 
   if (tid == 0) {
     ctl.abort = 0;
     ctl.status = g.status;
-    for (int s = 0; s < kSlots; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 2); mbar_init(clean(s), 1); }   // read by the MMAs, passed by the clearing warp
+    for (int s = 0; s < kSlots; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1);
-      mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 256); mbar_init(p_full(s, 1), 256); mbar_init(o_full(s), 1);
+      mbar_init(q_full(s), 1);
+      mbar_init(s_full(s), 1); mbar_init(p_full(s, 0), 256 + 1); mbar_init(p_full(s, 1), 256); mbar_init(o_full(s), 1);
       mbar_init(piece_full(s), 1); mbar_init(piece_empty(s), kItemReaders);
     }
     fence_mbar_init();
@@ -338,14 +349,22 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     return row0 + kTileKeys > p.kv_end || (row0 < p.win_lo && row0 + kTileKeys > g.n_sink);
   };
 
-  if (warp == kSchedWarp) {
-    // ------------------------------------------------------------ scheduler: which piece is next, and what it is
+  if (warp == kProducerWarp) {
+    // ------------------------------------------------------------ the pieces of work, and their K and V: a copy per page box and half of
+    // the columns
+    if (lane == 0) { tma_prefetch_desc(&k_map); tma_prefetch_desc(&v_map); }
+    const int copies = 2 * (kTileKeys >> a.lg_box);
+    const uint32_t box_bytes = (uint32_t)a.box_rows * kLineBytes;
+    const int box = lane >> 1, half = lane & 1;
+    int slot = 0;
+    uint32_t ph = 1;                         // parity of a slot's emptiness
     const long long heavy_work = (long long)n_heavy_pieces * g.Hkv, total = heavy_work + (long long)n_tiles * g.Hkv;
     long long w = blockIdx.x;
     int at_heavy = 0;
     int strip = -32, strip_first = 0, strip_all = 0, incl = 0, nt = 0, s0 = 0, n = 0, kv = 0;   // 32 sequences, one a lane
     uint32_t n_given = 0;
-    for (;;) {
+    bool ok = true;
+    while (ok) {
       const bool more = w < total;
       Piece p;
       p.n_steps = 0;
@@ -427,18 +446,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         break;
       }
       w = __shfl_sync(0xffffffffu, next, 0);
-    }
-  } else if (warp == kProducerWarp) {
-    // ------------------------------------------------------------ K and V, a copy per page box and half of the columns
-    if (lane == 0) { tma_prefetch_desc(&k_map); tma_prefetch_desc(&v_map); }
-    const int copies = 2 * (kTileKeys >> a.lg_box);
-    const uint32_t box_bytes = (uint32_t)a.box_rows * kLineBytes;
-    const int box = lane >> 1, half = lane & 1;
-    int slot = 0;
-    uint32_t ph = 1;                         // parity of a slot's emptiness
-    bool ok = true;
-    Piece it;
-    while (ok && take_piece(it)) {
+      const Piece& it = p;
       const int h = it.head;
       const int* table = a.block_table + (size_t)it.seq * g.max_pages;
       int ids = 0, ids_at = -1;
@@ -471,36 +479,50 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         }
       }
     }
-  } else if (warp == kQWarp) {
-    // ------------------------------------------------------------ the query blocks of the streams; unseen rows of V
+  } else if (warp == kStewardWarp) {
+    // ------------------------------------------------------------ steward: the query blocks, unseen rows of V, and all that the warp which
+    // issues the MMAs would otherwise wait for or report: it shares its scheduler with busy warps, and each of those waits and commits
+    // cost it 100 cycles and more, during which the tensor cores ran dry (3600 cycles a step with all of them).
+    // For step j it answers for V(j) and K(j+1) having landed by being one of those that hand over P; and as MMAs complete in
+    // order, S(j) of the last stream tells it that K(j) and V(j-1) have been read.
     if (lane == 0) tma_prefetch_desc(&q_map);
-    uint32_t ph[2] = {1u, 1u}, rph = 0;
-    int slot = 0;                            // the ring holds K and V in turn
+    uint32_t rph = 0, sph = 0, pph = 3u, oph = 0;     // parities: of the ring; a bit for each stream
+    int slot = 0;                            // of the next tile to land
     bool ok = true;
-    Piece it;
-    while (ok && take_piece(it)) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (s * R >= it.n_tok) break;
-        ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, q_empty(s), ph[s], 0x200u));
-        if (!ok) break;
-        ph[s] ^= 1u;
-        if (lane == 0) {
+    auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) {
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, bar, parity, code));
+    };
+    auto landed = [&]() {
+      const int sl = slot;
+      wait(full(sl), rph, 0x280u);
+      if (++slot == kSlots) { slot = 0; rph ^= 1u; }
+      return sl;
+    };
+    auto release = [&](int sl) { if (ok && lane == 0) mbar_arrive(empty(sl)); };
+    auto load_q = [&](const Piece& p) {
+      if (lane == 0)
+        for (int s = 0; s < 2 && s * R < p.n_tok; ++s) {
           mbar_arrive_expect_tx(q_full(s), 2u * (uint32_t)(R * g.G) * kLineBytes);
           for (int half = 0; half < 2; ++half)
-            tma_load_4d(q_base + s * kTileBytes + half * (kTileBytes / 2), &q_map, q_full(s), half * kHalfCols, 0, it.head, it.tok0 + s * R);
+            tma_load_4d(q_base + s * kTileBytes + half * (kTileBytes / 2), &q_map, q_full(s), half * kHalfCols, 0, p.head, p.tok0 + s * R);
         }
-        __syncwarp();
-      }
-      // Rows of V that none of the tokens sees may hold anything (or have not been loaded), and zero times that could be a NaN: they
-      // become zeros before the product.  (Done by the issuing warp, a tile of a window's border or a prompt's end cost it 2500 cycles.)
-      // Every tile of the ring passes here, so that this warp is never a round of the ring behind or ahead of it.
-      for (int f = 0; ok && f < 2 * it.n_steps; ++f) {
-        ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, full(slot), rph, 0x280u));
-        if (!ok) break;
-        const int row0 = step_row(it, f >> 1);
-        if ((f & 1) && unseen_rows(it, row0)) {
-          unsigned char* const mine = smem_al + (2 + slot) * kTileBytes + ((lane >> 3) & 1) * (kTileBytes / 2) + (lane & 7) * 16;
+      __syncwarp();
+    };
+    Piece it, next;
+    bool more = take_piece(it);
+    if (more) load_q(it);
+    while (ok && more) {
+      const int n = it.n_steps, last = it.n_tok > R ? 1 : 0;
+      const uint32_t streams = last ? 3u : 1u;
+      int ks = landed(), vs = 0;
+      for (int j = 0; ok && j < n; ++j) {
+        const int ks_read = ks, vs_read = vs;
+        vs = landed();
+        const int row0 = step_row(it, j);
+        if (unseen_rows(it, row0)) {
+          // Rows of V that none of the tokens sees may hold anything (or have not been loaded), and zero times that could be a NaN: they
+          // become zeros before the product.
+          unsigned char* const mine = smem_al + (2 + vs) * kTileBytes + ((lane >> 3) & 1) * (kTileBytes / 2) + (lane & 7) * 16;
           auto clear = [&](int r0, int r1) {
 #pragma unroll 4
             for (int r = max(r0, 0) + (lane >> 4); r < min(r1, kTileKeys); r += 2)
@@ -508,16 +530,32 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           };
           clear(it.kv_end - row0, kTileKeys);
           clear(g.n_sink - row0, min(it.win_lo, it.kv_end) - row0);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(clean(slot));
         }
-        if (lane == 0) mbar_arrive(empty(slot));
-        if (++slot == kSlots) { slot = 0; rph ^= 1u; }
+        if (j + 1 < n) ks = landed();
+        fence_proxy_async_smem();
+        __syncwarp();
+        for (int s = 0; s <= last; ++s) {
+          wait(p_full(s, 0), (pph >> s) & 1u, 0x220u);      // (that of the step before, so that this arrival counts for its own)
+          if (ok && lane == 0) mbar_arrive(p_full(s, 0));
+        }
+        pph ^= streams;
+        wait(s_full(last), (sph >> last) & 1u, 0x210u);
+        sph ^= streams;
+        release(ks_read);
+        if (j > 0) release(vs_read);
       }
+      // the next piece's queries, while the last step of this one is under way
+      more = ok && take_piece(next);
+      if (more) load_q(next);
+      wait(o_full(last), (oph >> last) & 1u, 0x230u);
+      oph ^= streams;
+      release(vs);
+      it = next;
     }
   } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------ all MMAs, the warp as a whole with one lane issuing
+    // ------------------------------------------------------------ all MMAs, the warp as a whole with one lane issuing.  The streams take
+    // turns, which also keeps one half a step behind the other (with a warp each they fell into step, both at their softmax and then both
+    // waiting for the tensor cores: 4000 cycles a step instead of 2970).
     constexpr uint32_t kTypes = kF16 ? ~((7u << 7) | (7u << 10)) : ~0u;    // f16 operands are type 0
     const uint32_t idesc_s = umma_idesc(128, 128, false, false) & kTypes;   // A = Q, B = K tile, both K-major
     const uint32_t idesc_o = umma_idesc(128, 128, false, true) & kTypes;    // A = P (tensor memory), B = V tile, MN-major
@@ -526,12 +564,12 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     const uint64_t dv = smem_desc_sw128(ring, kTileBytes / 2, 1024u);
     const bool leader = elect_one();
     int slot = 0;
-    uint32_t ph = 0, qph[2] = {0u, 0u}, pph[2] = {0u, 0u};
-    bool ok = true;
-    auto take = [&](int& sl) {              // the next tile of the ring, landed
-      sl = slot;
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, full(slot), ph, 0x300u));
-      if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+    uint32_t ph = 0, qph = 0, pph = 0;       // parities: of the ring; a bit for each stream
+    auto advance = [&]() { if (++slot == kSlots) { slot = 0; ph ^= 1u; } };
+    auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) {
+      const bool ok = __any_sync(0xffffffffu, mbar_try_wait(bar, parity)) || __all_sync(0xffffffffu, mbar_wait_poll_far(&ctl, bar, parity, code));
+      tc_fence_after_sync();
+      return ok;
     };
     auto issue_s = [&](int s, int k_slot) {
       if (leader) {
@@ -546,78 +584,48 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       }
       __syncwarp();
     };
-    // P V of the keys of part 0 (0..31 and 64..95 of the tile) or 1; the P of keys 64.. sits at columns 64..
-    auto issue_pv = [&](int s, int v_slot, int part, bool first) {
-      if (leader) {
-        const uint32_t d = tmem_base + kColO + (uint32_t)(s * 128), p = tmem_base + (uint32_t)(s * 128);
-        const uint64_t vd = desc_advance(dv, (uint32_t)v_slot * kTileBytes);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int kk = (i >> 1) * 4 + (i & 1);           // the step of part 0; that of part 1 is two on
-          const uint32_t col = p + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8) + (part ? 16u : 0u);
-          const uint64_t v = desc_advance(vd, ((uint32_t)kk + (part ? 2u : 0u)) * 16u * kLineBytes);
-          if (i == 0) umma_ts(d, col, v, idesc_o, first ? 0u : 1u);
-          else umma_ts_imm<1>(d, col, v, idesc_o);
-        }
-      }
-      __syncwarp();
+    // P V of 16 keys of each half of the tile: steps kk and kk + 4; the P of keys 64.. sits at columns 64..
+    auto pv = [&](int s, uint64_t vd, int kk, uint32_t acc) {
+      const uint32_t p = tmem_base + (uint32_t)(s * 128 + kk * 8), d = tmem_base + (uint32_t)(s * 128) + kColO;
+      umma_ts(d, p, desc_advance(vd, (uint32_t)kk * 16u * kLineBytes), idesc_o, acc);
+      umma_ts_imm<1>(d, p + 64u, desc_advance(vd, (uint32_t)(kk + 4) * 16u * kLineBytes), idesc_o);
     };
-    auto commit = [&](uint32_t bar) {
-      if (leader) umma_commit(bar);
-      __syncwarp();
-    };
-    uint32_t cleaned = 0;                   // parity of each slot's barrier
     Piece it;
-    while (ok && take_piece(it)) {
-      const bool dual = it.n_tok > R;
-      const int n = it.n_steps;
-      int ks, vs;
-      for (int s = 0; s < 2; ++s) {
-        if (s == 1 && !dual) break;
-        ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, q_full(s), qph[s], 0x400u));
-        qph[s] ^= 1u;
-        if (s == 0) take(ks);
-        if (!ok) break;
-        tc_fence_after_sync();
-        issue_s(s, ks);
-        if (n == 1) commit(q_empty(s));
+    while (take_piece(it)) {
+      const int n = it.n_steps, n_streams = it.n_tok > R ? 2 : 1;
+      if (!wait(full(slot), ph, 0x300u)) break;
+      bool ok = true;
+      for (int s = 0; ok && s < n_streams; ++s) {
+        ok = wait(q_full(s), (qph >> s) & 1u, 0x400u);
+        qph ^= 1u << s;
+        if (ok) issue_s(s, slot);
+      }
+      advance();
+      for (int j = 0; ok && j < n; ++j) {
+        const uint64_t vd = desc_advance(dv, (uint32_t)slot * kTileBytes);
+        advance();
+        const bool more = j + 1 < n;
+        for (int s = 0; s < n_streams; ++s) {
+          const uint32_t parity = (pph >> s) & 1u;
+          if (!(ok = wait(p_full(s, 0), parity, 0x500u))) break;
+          if (leader) {
+            pv(s, vd, 0, j ? 1u : 0u);
+            pv(s, vd, 1, 1u);
+            pv(s, vd, 2, 1u);
+          }
+          __syncwarp();
+          if (!(ok = wait(p_full(s, 1), parity, 0x510u))) break;
+          if (leader) {
+            pv(s, vd, 3, 1u);
+            if (!more) umma_commit(o_full(s));
+          }
+          __syncwarp();
+          if (more) issue_s(s, slot);
+          pph ^= 1u << s;
+        }
+        if (more) advance();
       }
       if (!ok) break;
-      commit(empty(ks));
-      for (int j = 0; j < n; ++j) {
-        take(vs);
-        if (!ok) break;
-        if (unseen_rows(it, step_row(it, j))) {
-          ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, clean(vs), (cleaned >> vs) & 1u, 0x380u));
-          cleaned ^= 1u << vs;
-          if (!ok) break;
-        }
-        const bool more = j + 1 < n;
-        for (int s = 0; s < 2; ++s) {
-          if (s == 1 && !dual) break;
-          ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, p_full(s, 0), pph[s], 0x500u));
-          if (!ok) break;
-          tc_fence_after_sync();
-          issue_pv(s, vs, 0, j == 0);
-          ok = __all_sync(0xffffffffu, mbar_wait_far(&ctl, p_full(s, 1), pph[s], 0x580u));
-          pph[s] ^= 1u;
-          if (!ok) break;
-          tc_fence_after_sync();
-          issue_pv(s, vs, 1, false);
-          if (!more) {
-            commit(o_full(s));
-          } else {
-            if (s == 0) take(ks);
-            if (!ok) break;
-            tc_fence_after_sync();
-            issue_s(s, ks);
-            if (j + 2 == n) commit(q_empty(s));
-          }
-        }
-        if (!ok) break;
-        commit(empty(vs));
-        if (more) commit(empty(ks));
-      }
     }
   } else if (warp < kSoftmaxWarps) {
     // ------------------------------------------------------------ softmax: two threads to a row
@@ -655,17 +663,6 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         m[1] = max3(m[1], __uint_as_float(x[c + 2]), __uint_as_float(x[c + 3]));
       }
       return max3(fmaxf(m[0], m[1]), __uint_as_float(x[30]), __uint_as_float(x[31]));
-    };
-    // exp2(scale2 x - ref) of 32 keys, rounded in pairs, and their sum
-    auto terms = [&](const uint32_t (&x)[32], float ref, uint32_t (&packed)[16], f32x2& sum) {
-      const f32x2 nref = pack2(ref == -INFINITY ? 0.f : -ref);
-#pragma unroll
-      for (int c = 0; c < 32; c += 2) {
-        const f32x2 y = exp2_pair<false>(fma2(pack2(x[c], x[c + 1]), sc, nref), c / 2);
-        sum = add2(sum, y);
-        const float2 p = unpack2(y);
-        packed[c >> 1] = pack16<kF16>(p.x, p.y);
-      }
     };
     uint32_t sph = 0, oph = 0;
     // The warps of a stream meet at barriers, so they leave the loop together, and a wait that runs out (after which all others
@@ -741,14 +738,16 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           }
         }
         f32x2 sum = 0ull;
-        terms(x, ref, packed, sum);
+        terms<kF16, 0, 32>(x, sc, ref, packed, sum);
         tmem_st16(s_addr, packed);
+        tmem_ld32(s_addr + 32, x);
+        terms<kF16, 0, 16>(x, sc, ref, packed, sum);
+        tmem_st8(s_addr + 16, packed);
         tmem_st_wait();
         tc_fence_before_sync();
         mbar_arrive(p_full(s, 0));
-        tmem_ld32(s_addr + 32, x);
-        terms(x, ref, packed, sum);
-        tmem_st16(s_addr + 16, packed);
+        terms<kF16, 16, 32>(x, sc, ref, packed, sum);
+        tmem_st8(s_addr + 24, packed);
         tmem_st_wait();
         tc_fence_before_sync();
         mbar_arrive(p_full(s, 1));
