@@ -139,7 +139,7 @@ struct Partial {
 // Rows `row(i)` of n partial rows of kStride floats, this lane's four outputs of each, joined in order.
 template <typename Row>
 __device__ __forceinline__ void join_rows(Partial& p, int n, int lane, Row row) {
-  constexpr int kBatch = 4;   // loads in flight
+  constexpr int kBatch = 8;   // loads in flight
   for (int i0 = 0; i0 < n; i0 += kBatch) {
     float4 o[kBatch];
     float2 ml[kBatch];

@@ -229,6 +229,10 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         if (++slot == kSlots) { slot = 0; ph ^= 1u; }
       }
     } while (next_unit());
+    if (*abort_flag) {      // a wait has run out: copies may still be under way, and need this CTA's memory for a few microseconds
+      const long long t0 = clock64();
+      while (clock64() - t0 < 400000) {}
+    }
     return;
   }
 

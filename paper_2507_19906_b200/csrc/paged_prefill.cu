@@ -37,7 +37,7 @@ constexpr int kThreads = 640;
 constexpr int kSlots = 5;                         // K and V tiles in one ring, in the order in which they are used
 constexpr int kTileBytes = kKvTileBytes;          // 32 KB
 constexpr uint32_t kColO = 256;
-constexpr int kMaxHeavy = 2 * kSms;               // tiles of at least half an SM's mean share
+constexpr int kMaxHeavy = 2 * kSms + kSms / 2;    // tiles of at least half an SM's mean share, and those of a ragged last round
 constexpr int kItemReaders = kSoftmaxWarps + 2;   // warps that take a piece from the producer
 
 // A piece of work: a tile of rows of one kv head against a range of steps.
@@ -157,6 +157,170 @@ __device__ __forceinline__ void terms(const uint32_t (&x)[32], f32x2 scale2, flo
   }
 }
 
+// The list of work: heavy tiles and those of a ragged last round, in falling order of their chunks, at a.heavy; made by all threads of
+// the CTA in `scratch`.  (By one warp for small batches: 4 us instead of 2.)
+struct WorkList {
+  int n_tiles, n_heavy_pieces;
+  unsigned long long all_steps;    // of all tiles and heads
+  int tail_from;                   // tiles from here on are cut into tail_chunks
+  int tail_chunks;
+  // Pieces of like size that fill a few rounds of the SMs and a bit leave most SMs idle in the last round: the tiles of that bit are
+  // cut so that their chunks fill it.  (312 pieces of 14 steps: 102 us.)
+  __device__ __forceinline__ bool in_tail(const KernelArgs& a, int e, int n) const {
+    return e >= tail_from && 10ull * n * n_tiles * a.g.Hkv >= 6 * all_steps;     // (not those far below the mean)
+  }
+  __device__ __forceinline__ int chunks(const KernelArgs& a, int e, int n, int rows) const {
+    if (!in_tail(a, e, n)) return chunks_of(a, n, rows, all_steps);
+    const int k = max(1, min(min(tail_chunks, n / 3), (int)sqrtf(375.f * n / rows))), len = (n + k - 1) / k;
+    return (n + len - 1) / len;
+  }
+  __device__ __forceinline__ bool listed(const KernelArgs& a, int e, int n) const { return is_heavy(n, all_steps) || in_tail(a, e, n); }
+};
+__device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* scratch, int tid) {
+  const PagedGeom& g = a.g;
+  constexpr int kN = kThreads, kWarps = kN / 32;
+  const int lane = tid & 31, warp = tid >> 5;
+  const int size = 2 * a.tokens;
+  int* const tb = reinterpret_cast<int*>(scratch);                    // [n_seqs + 1]: first tiles of the sequences
+  int* const sums = tb + kMaxSequences + 1;                           // [63]
+  int2* const found = reinterpret_cast<int2*>(sums + 63);             // [kMaxHeavy] {tile, steps of a chunk}
+  int2* const order = found + kMaxHeavy;                              // by rank: {chunks, rows of a head}
+  Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
+  auto scan = [&](int v, int& all) {       // what lies ahead of this thread, and the sum
+    int incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const int u = sums[w];
+      if (w < warp) before += u;
+      all += u;
+    }
+    return before + incl - v;
+  };
+  WorkList r{0, 0, 0, 0x7fffffff, 1};
+  for (int base = 0; base < a.n_seqs; base += kN) {
+    const int b = base + tid;
+    int nt = 0, all;
+    if (b < a.n_seqs) {
+      int s0, n, kv;
+      if (lengths(a, b, s0, n, kv) && blockIdx.x == 0) paged_flag(g.status, kBadLength);
+      nt = (n + size - 1) / size;
+    }
+    const int before = scan(nt, all);
+    if (b < a.n_seqs) tb[b] = r.n_tiles + before;
+    r.n_tiles += all;
+  }
+  if (tid == 0) tb[a.n_seqs] = r.n_tiles;
+  __syncthreads();
+  auto tile_of = [&](int e, Piece& p) {
+    int lo = 0, hi = a.n_seqs;             // tb[lo] <= e < tb[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tb[mid] <= e) lo = mid; else hi = mid;
+    }
+    int s0, n, kv;
+    lengths(a, lo, s0, n, kv);
+    tile_piece(a, lo, s0, n, kv, e - tb[lo], p);
+  };
+  unsigned long long steps = 0;
+  int my_steps = 0;             // of tile tid
+  for (int e = tid; e < r.n_tiles; e += kN) {
+    Piece p;
+    tile_of(e, p);
+    steps += (unsigned)p.n_steps;
+    if (e == tid) my_steps = p.n_steps;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
+  unsigned long long* const wide = reinterpret_cast<unsigned long long*>(found);
+  if (lane == 0) wide[warp] = steps;
+  __syncthreads();
+  steps = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) steps += wide[w];
+  __syncthreads();
+  r.all_steps = steps * (unsigned long long)g.Hkv;
+  const long long all_pieces = (long long)r.n_tiles * g.Hkv;
+  if (!a.partial && all_pieces > gridDim.x && all_pieces < 5 * gridDim.x) {
+    const int left = (int)(all_pieces % gridDim.x), n_tail = (left + g.Hkv - 1) / g.Hkv;
+    if (left > 0 && 2 * n_tail * g.Hkv <= gridDim.x) {
+      r.tail_from = r.n_tiles - n_tail;
+      r.tail_chunks = (int)gridDim.x / (n_tail * g.Hkv);
+    }
+  }
+  // heavy tiles, in the order of the tiles
+  int n_heavy = 0;
+  for (int base = 0; base < r.n_tiles; base += kN) {
+    const int e = base + tid;
+    bool is = false;
+    if (e < r.n_tiles) {
+      if (base) {
+        Piece p;
+        tile_of(e, p);
+        my_steps = p.n_steps;
+      }
+      is = r.listed(a, e, my_steps);
+    }
+    int all;
+    const int i = n_heavy + scan(is ? 1 : 0, all);
+    if (is && i < kMaxHeavy) found[i] = make_int2(e, 0);
+    n_heavy += all;
+  }
+  n_heavy = min(n_heavy, kMaxHeavy);   // (there are no more)
+  if (n_heavy == 0) return r;
+  // ... the heaviest first
+  __syncthreads();
+  for (int i = tid; i < n_heavy; i += kN) {
+    Piece p;
+    tile_of(found[i].x, p);
+    const int k = r.chunks(a, found[i].x, p.n_steps, p.n_tok * g.G);
+    found[i].y = (p.n_steps + k - 1) / k;
+  }
+  __syncthreads();
+  for (int i = tid; i < n_heavy; i += kN) {
+    Piece p;
+    tile_of(found[i].x, p);
+    const int len = found[i].y, k = (p.n_steps + len - 1) / len;
+    int rank = i;
+    if (a.n_seqs > 1) {                // (one sequence's are in order)
+      rank = 0;
+      for (int j = 0; j < n_heavy; ++j) {
+        const int l = found[j].y;
+        rank += l > len || (l == len && j < i);
+      }
+    }
+    order[rank] = make_int2(k, p.n_tok * g.G);
+    heavy[rank] = Heavy{p.seq, found[i].x - tb[p.seq], k, len, 0, 0, 0, 0};
+  }
+  __syncthreads();
+  int pieces = 0, rows = a.partial ? g.n_tokens * g.Hq : 0, counters = 0;
+  for (int base = 0; base < n_heavy; base += kN) {
+    const int i = base + tid;
+    const int2 o = i < n_heavy ? order[i] : make_int2(0, 0);
+    const bool cut = o.x > 1;
+    int all_pieces, all_rows, all_counters;
+    const int p0 = scan(o.x, all_pieces), r0 = scan(cut ? o.x * g.Hkv * o.y : 0, all_rows), c0 = scan(cut ? 2 * g.Hkv : 0, all_counters);
+    if (i < n_heavy) {
+      heavy[i].first_piece = pieces + p0;
+      heavy[i].part_row = rows + r0;
+      heavy[i].counter = counters + c0;
+    }
+    pieces += all_pieces; rows += all_rows; counters += all_counters;
+  }
+  r.n_heavy_pieces = pieces;
+  __syncthreads();
+  return r;
+}
+
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -203,133 +367,12 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   pdl_wait();
   const int R = a.tokens;
 
-  // ---- the list of work, the same in every CTA: first tiles of the sequences, all steps, heavy tiles
-  int* const tb = reinterpret_cast<int*>(smem_al + 2 * kTileBytes);   // [n_seqs + 1], where the ring will be
-  int* const sums = tb + kMaxSequences + 1;                           // [32] and a count
-  int2* const found = reinterpret_cast<int2*>(sums + 63);             // [kMaxHeavy] {tile, steps}
-  Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
+  // ---- the list of work, the same in every CTA; only the producer needs it
   const int size = 2 * R;
-  auto block_sum = [&](int incl, int& before) {      // of inclusive warp sums: their total, and what lies ahead of this warp
-    __syncthreads();
-    if (lane == 31) sums[warp] = incl;
-    __syncthreads();
-    int all = 0;
-    before = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-      const int v = sums[w];
-      if (w < warp) before += v;
-      all += v;
-    }
-    return all;
-  };
-  int n_tiles = 0;
-  for (int base = 0; base < a.n_seqs; base += kThreads) {
-    const int b = base + tid;
-    int nt = 0;
-    if (b < a.n_seqs) {
-      int s0, n, kv;
-      if (lengths(a, b, s0, n, kv) && blockIdx.x == 0) paged_flag(g.status, kBadLength);
-      nt = (n + size - 1) / size;
-    }
-    int incl = nt, before;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    const int all = block_sum(incl, before);
-    if (b < a.n_seqs) tb[b] = n_tiles + before + incl - nt;
-    n_tiles += all;
-  }
-  if (tid == 0) tb[a.n_seqs] = n_tiles;
+  const WorkList work = make_list(a, smem_al + 2 * kTileBytes, tid);
   if (a.partial)      // tokens of no group have no partial rows
     for (int t = blockIdx.x * kThreads + tid; t < g.n_tokens; t += gridDim.x * kThreads)
       if (t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs)) a.token_parts[t] = PagedToken{0, 0, 0, 0};
-  __syncthreads();
-  auto tile_of = [&](int e, Piece& p) {
-    int lo = 0, hi = a.n_seqs;             // tb[lo] <= e < tb[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tb[mid] <= e) lo = mid; else hi = mid;
-    }
-    int s0, n, kv;
-    lengths(a, lo, s0, n, kv);
-    tile_piece(a, lo, s0, n, kv, e - tb[lo], p);
-  };
-  unsigned long long steps = 0;
-  int my_steps = 0;             // of tile tid
-  for (int e = tid; e < n_tiles; e += kThreads) {
-    Piece p;
-    tile_of(e, p);
-    steps += (unsigned)p.n_steps;
-    if (e == tid) my_steps = p.n_steps;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
-  unsigned long long* const wide = reinterpret_cast<unsigned long long*>(found);
-  if (lane == 0) wide[warp] = steps;
-  __syncthreads();
-  unsigned long long all_steps = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) all_steps += wide[w];
-  all_steps *= (unsigned long long)g.Hkv;
-  __syncthreads();
-  // heavy tiles, in the order of the tiles
-  int n_heavy = 0;
-  for (int base = 0; base < n_tiles; base += kThreads) {
-    const int e = base + tid;
-    bool is = false;
-    if (e < n_tiles) {
-      if (base) {
-        Piece p;
-        tile_of(e, p);
-        my_steps = p.n_steps;
-      }
-      is = is_heavy(my_steps, all_steps);
-    }
-    if (!__syncthreads_or(is)) continue;
-    const unsigned m = __ballot_sync(0xffffffffu, is);
-    int before;
-    const int all = block_sum(__popc(m), before);
-    const int i = n_heavy + before + __popc(m & ((1u << lane) - 1u));
-    if (is && i < kMaxHeavy) found[i] = make_int2(e, 0);
-    n_heavy += all;
-  }
-  n_heavy = min(n_heavy, kMaxHeavy);   // (there are no more)
-  // ... the heaviest first
-  int n_heavy_pieces = 0;
-  if (n_heavy) {
-    __syncthreads();
-    int2* const order = found + kMaxHeavy;     // by rank: {chunks, rows of a head}
-    Piece p;
-    int k = 0, len = 0, rank = 0;
-    if (tid < n_heavy) {
-      tile_of(found[tid].x, p);
-      k = chunks_of(a, p.n_steps, p.n_tok * g.G, all_steps);
-      len = (p.n_steps + k - 1) / k;
-      found[tid].y = len;
-    }
-    __syncthreads();
-    if (tid < n_heavy) {
-      for (int j = 0; j < n_heavy; ++j) {
-        const int l = found[j].y;
-        rank += l > len || (l == len && j < tid);
-      }
-      order[rank] = make_int2(k, p.n_tok * g.G);
-    }
-    __syncthreads();
-    if (tid < n_heavy) {
-      Heavy x{p.seq, found[tid].x - tb[p.seq], k, len, 0, a.partial ? g.n_tokens * g.Hq : 0, 0, 0};
-      for (int j = 0; j < rank; ++j) {
-        const int2 o = order[j];
-        x.first_piece += o.x;
-        if (o.x > 1) { x.part_row += o.x * g.Hkv * o.y; x.counter += 2 * g.Hkv; }
-      }
-      heavy[rank] = x;
-    }
-    for (int j = 0; j < n_heavy; ++j) n_heavy_pieces += order[j].x;
-  }
   fence_proxy_async_smem();    // the ring's copies come after what was written there
   __syncthreads();
 
@@ -359,7 +402,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     const int box = lane >> 1, half = lane & 1;
     int slot = 0;
     uint32_t ph = 1;                         // parity of a slot's emptiness
-    const long long heavy_work = (long long)n_heavy_pieces * g.Hkv, total = heavy_work + (long long)n_tiles * g.Hkv;
+    const Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
+    const long long heavy_work = (long long)work.n_heavy_pieces * g.Hkv, total = heavy_work + (long long)work.n_tiles * g.Hkv;
     long long w = blockIdx.x;
     int at_heavy = 0;
     int strip = -32, strip_first = 0, strip_all = 0, incl = 0, nt = 0, s0 = 0, n = 0, kv = 0;   // 32 sequences, one a lane
@@ -376,7 +420,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const int piece = (int)(w / g.Hkv);
           p.head = (int)(w - (long long)piece * g.Hkv);
           Heavy x;
-          for (;; ++at_heavy) {
+          for (; at_heavy < kMaxHeavy; ++at_heavy) {
             const int4* src = reinterpret_cast<const int4*>(heavy + at_heavy);
             *reinterpret_cast<int4*>(&x) = __ldcg(src);
             *(reinterpret_cast<int4*>(&x) + 1) = __ldcg(src + 1);
@@ -420,7 +464,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const int h = p.head, t = e - strip_first - __shfl_sync(0xffffffffu, incl - nt, own);
           tile_piece(a, strip + own, __shfl_sync(0xffffffffu, s0, own), __shfl_sync(0xffffffffu, n, own), __shfl_sync(0xffffffffu, kv, own), t, p);
           p.head = h;
-          if (is_heavy(p.n_steps, all_steps)) {     // it was among those
+          if (work.listed(a, e, p.n_steps)) {     // it was among those
             w = __shfl_sync(0xffffffffu, next, 0);
             continue;
           }
@@ -484,22 +528,17 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     // ------------------------------------------------------------ steward: the query blocks, unseen rows of V, and all that the warp which
     // issues the MMAs would otherwise wait for or report: it shares its scheduler with busy warps, and each of those waits and commits
     // cost it 100 cycles and more, during which the tensor cores ran dry (3600 cycles a step with all of them).
-    // For step j it answers for V(j) and K(j+1) having landed by being one of those that hand over P; and as MMAs complete in
-    // order, S(j) of the last stream tells it that K(j) and V(j-1) have been read.
+    // For step j it answers for V(j) and K(j+1) having landed by being one of those that hand over P.  It waits for nothing that could
+    // go on without it, so that no phase of a barrier can pass it by: a tile of the ring is given back (by the softmax of the last
+    // stream, which is told of S(j) when K(j) and V(j-1) have been read) only after a product that needed its answer.
     if (lane == 0) tma_prefetch_desc(&q_map);
-    uint32_t rph = 0, sph = 0, pph = 3u, oph = 0;     // parities: of the ring; a bit for each stream
+    uint32_t rph = 0, pph = 3u;              // parities: of the ring; a bit for each stream
     int slot = 0;                            // of the next tile to land
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) {
       ok = ok && __all_sync(0xffffffffu, mbar_wait_far(&ctl, bar, parity, code));
     };
-    auto landed = [&]() {
-      const int sl = slot;
-      wait(full(sl), rph, 0x280u);
-      if (++slot == kSlots) { slot = 0; rph ^= 1u; }
-      return sl;
-    };
-    auto release = [&](int sl) { if (ok && lane == 0) mbar_arrive(empty(sl)); };
+    auto advance = [&]() { if (++slot == kSlots) { slot = 0; rph ^= 1u; } };
     auto load_q = [&](const Piece& p) {
       if (lane == 0)
         for (int s = 0; s < 2 && s * R < p.n_tok; ++s) {
@@ -509,18 +548,17 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         }
       __syncwarp();
     };
-    Piece it, next;
-    bool more = take_piece(it);
-    if (more) load_q(it);
-    while (ok && more) {
+    Piece it;
+    while (ok && take_piece(it)) {
+      load_q(it);                            // (all products with the queries of the piece before are done: see below)
       const int n = it.n_steps, last = it.n_tok > R ? 1 : 0;
-      const uint32_t streams = last ? 3u : 1u;
-      int ks = landed(), vs = 0;
+      advance();                             // K(0): the issuing warp waits for it itself
       for (int j = 0; ok && j < n; ++j) {
-        const int ks_read = ks, vs_read = vs;
-        vs = landed();
+        const int vs = slot;
+        wait(full(vs), rph, 0x280u);
+        advance();
         const int row0 = step_row(it, j);
-        if (unseen_rows(it, row0)) {
+        if (ok && unseen_rows(it, row0)) {
           // Rows of V that none of the tokens sees may hold anything (or have not been loaded), and zero times that could be a NaN: they
           // become zeros before the product.
           unsigned char* const mine = smem_al + (2 + vs) * kTileBytes + ((lane >> 3) & 1) * (kTileBytes / 2) + (lane & 7) * 16;
@@ -532,26 +570,20 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           clear(it.kv_end - row0, kTileKeys);
           clear(g.n_sink - row0, min(it.win_lo, it.kv_end) - row0);
         }
-        if (j + 1 < n) ks = landed();
+        if (j + 1 < n) {
+          wait(full(slot), rph, 0x290u);
+          advance();
+        }
         fence_proxy_async_smem();
         __syncwarp();
         for (int s = 0; s <= last; ++s) {
           wait(p_full(s, 0), (pph >> s) & 1u, 0x220u);      // (that of the step before, so that this arrival counts for its own)
           if (ok && lane == 0) mbar_arrive(p_full(s, 0));
+          pph ^= 1u << s;
         }
-        pph ^= streams;
-        wait(s_full(last), (sph >> last) & 1u, 0x210u);
-        sph ^= streams;
-        release(ks_read);
-        if (j > 0) release(vs_read);
       }
-      // the next piece's queries, while the last step of this one is under way
-      more = ok && take_piece(next);
-      if (more) load_q(next);
-      wait(o_full(last), (oph >> last) & 1u, 0x230u);
-      oph ^= streams;
-      release(vs);
-      it = next;
+      // the last stream hands over the P of the last step when its S, and so all S, are done: the queries may be replaced
+      wait(p_full(last, 0), (pph >> last) & 1u, 0x230u);
     }
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ all MMAs, the warp as a whole with one lane issuing.  The streams take
@@ -666,6 +698,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       return max3(fmaxf(m[0], m[1]), __uint_as_float(x[30]), __uint_as_float(x[31]));
     };
     uint32_t sph = 0, oph = 0;
+    int ring_at = 0;
     // The warps of a stream meet at barriers, so they leave the loop together, and a wait that runs out (after which all others
     // of the CTA return at once) takes none of them out of a piece.
     for (;;) {
@@ -679,7 +712,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         __syncwarp();
         if (lane == 0) mbar_arrive(piece_empty(slot));
       };
+      int ks = ring_at;                                // ring slot of K(j); V(j - 1) lies ahead of it
+      ring_at = (ring_at + 2 * n_steps) % kSlots;
       if (s * R >= it.n_tok) { give_back(); continue; }
+      const bool releases = (tid & 255) == 0 && (s + 1) * R >= it.n_tok;     // a thread of the last stream
+      auto release = [&](int sl) { mbar_arrive(empty(sl < 0 ? sl + kSlots : sl)); };
       const int pos = it.pos0 + i_tok;
       const int tok_last = min(it.n_tok, (s + 1) * R) - 1;
       // the keys from clear_lo (or from the first, as far as the sinks go) up to clear_hi are seen by all rows of the stream
@@ -693,6 +730,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         __syncwarp();
         sph ^= 1u;
         tc_fence_after_sync();
+        if (releases) {                                  // S(j) is done, and with it all MMAs issued before
+          release(ks);
+          if (j > 0) release(ks - 1);
+        }
+        ks = ks + 2 >= kSlots ? ks + 2 - kSlots : ks + 2;
         if (row0 + kTileKeys > clear_hi || (row0 < clear_lo && row0 + kTileKeys > g.n_sink)) {
           // keys that the row does not see become -inf where they lie, 16 columns at a time: in the registers, all unrolled, it was
           // code of 4 KB that few tiles need, and took 1500 cycles of each
@@ -757,6 +799,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       }
       mbar_wait(&ctl, o_full(s), oph, 0x700u);
       __syncwarp();
+      if (releases) release(ks - 1);                     // V of the last step
       oph ^= 1u;
       tc_fence_after_sync();
       // the row's sum, of the lower keys and the upper ones in this order
@@ -868,6 +911,10 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   }
   tc_fence_before_sync();
   __syncthreads();
+  if (ctl.abort) {      // a wait has run out: copies and MMAs may still be under way, and need this CTA's memory for a few microseconds
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000) {}
+  }
   pdl_trigger();
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
@@ -923,8 +970,9 @@ bool paged_kv_map(CUtensorMap* out, const void* base, const PagedGeom& g, int ro
 PagedWs paged_ws(int B, int Hq, int Hkv, int n_tokens, int n_groups) {
   PagedWs w{};
   const int G = Hq / Hkv;
-  // chunks of cut tiles are no more than the SMs; with a shared prefix every token has rows of its own in any case
-  w.max_rows = (long long)kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)n_tokens * Hq : 0);
+  // chunks of cut tiles are no more than the SMs, and as many again of a ragged last round; with a shared prefix every token has rows of its
+  // own in any case
+  w.max_rows = 2ll * kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)n_tokens * Hq : 0);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t off = kPagedPlan;
   w.sched = off;  off = up(off + (16 + 2 * kSms) * 4);
