@@ -135,9 +135,9 @@ __device__ __forceinline__ bool is_heavy(int n, unsigned long long all) { return
 // last CTA about 8 cycles a row and chunk, and a chunk less takes n / k steps of 3000 cycles off: beyond sqrt(375 n / rows) chunks
 // the joining costs more than it gives, and so it does for chunks of less than 8 steps (a shared prefix is joined elsewhere, by many).
 __device__ __forceinline__ int chunks_of(const KernelArgs& a, int n, int rows, unsigned long long all) {
-  const unsigned long long shares = (unsigned long long)n * gridDim.x / all;
+  const unsigned shares = all >> 31 ? 0u : (unsigned)n * gridDim.x / (unsigned)all;     // (n is below 2^23)
   if (shares < 2) return 1;
-  int k = (int)min(shares, (unsigned long long)n);
+  int k = min((int)shares, n);
   if (!a.partial) k = max(1, min(min(k, n / 8), (int)sqrtf(375.f * n / rows)));
   const int len = (n + k - 1) / k;
   return (n + len - 1) / len;
@@ -157,26 +157,174 @@ __device__ __forceinline__ void terms(const uint32_t (&x)[32], f32x2 scale2, flo
   }
 }
 
-// The list of work: heavy tiles and those of a ragged last round, in falling order of their chunks, at a.heavy; made by all threads of
-// the CTA in `scratch`.  (By one warp for small batches: 4 us instead of 2.)
+// The list of work: heavy tiles, or all of them where they make few rounds, in falling order of their chunks, at a.heavy; made by all threads of
+// the CTA in `scratch`, or for a few tiles by one warp.
 struct WorkList {
   int n_tiles, n_heavy_pieces;
   unsigned long long all_steps;    // of all tiles and heads
-  int tail_from;                   // tiles from here on are cut into tail_chunks
-  int tail_chunks;
-  // Pieces of like size that fill a few rounds of the SMs and a bit leave most SMs idle in the last round: the tiles of that bit are
-  // cut so that their chunks fill it.  (312 pieces of 14 steps: 102 us.)
-  __device__ __forceinline__ bool in_tail(const KernelArgs& a, int e, int n) const {
-    return e >= tail_from && 10ull * n * n_tiles * a.g.Hkv >= 6 * all_steps;     // (not those far below the mean)
+  bool every;                      // the list has all tiles
+  __device__ __forceinline__ bool listed(int n) const { return every || is_heavy(n, all_steps); }
+};
+
+// Few rounds of pieces (less than five, of tiles that fit the list) are all listed, so that they are dealt from the heaviest down, and those of them that
+// would begin a ragged last round are cut to fill it: of the tiles of at least 0.6 of the largest one's steps, those beyond whole
+// rounds, the last ones.  (312 pieces of 14 steps on 148 SMs: 102 us uncut.)
+struct Rounds {
+  int n_full, n_tail, tail_chunks;
+  __device__ __forceinline__ static bool is_full(int n, int n_max) { return 10 * n >= 6 * n_max; }
+  __device__ __forceinline__ void plan(const KernelArgs& a, int full) {
+    n_full = full;
+    n_tail = 0;
+    tail_chunks = 1;
+    const int left = full * a.g.Hkv % (int)gridDim.x, tail = (left + a.g.Hkv - 1) / a.g.Hkv;
+    if (a.partial || full * a.g.Hkv <= (int)gridDim.x || left == 0 || 2 * tail * a.g.Hkv > (int)gridDim.x) return;
+    n_tail = tail;
+    tail_chunks = (int)gridDim.x / (tail * a.g.Hkv);
   }
-  __device__ __forceinline__ int chunks(const KernelArgs& a, int e, int n, int rows) const {
-    if (!in_tail(a, e, n)) return chunks_of(a, n, rows, all_steps);
+  // chunks of a tile that is number `at` of the full ones, or (-1) none of them
+  __device__ __forceinline__ int chunks(const KernelArgs& a, int at, int n, int rows, unsigned long long all) const {
+    if (at < n_full - n_tail) return chunks_of(a, n, rows, all);
     const int k = max(1, min(min(tail_chunks, n / 3), (int)sqrtf(375.f * n / rows))), len = (n + k - 1) / k;
     return (n + len - 1) / len;
   }
-  __device__ __forceinline__ bool listed(const KernelArgs& a, int e, int n) const { return is_heavy(n, all_steps) || in_tail(a, e, n); }
 };
-__device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* scratch, int tid) {
+__device__ __forceinline__ bool few_rounds(const KernelArgs& a, int n_tiles) {
+  return n_tiles <= kMaxHeavy && (long long)n_tiles * a.g.Hkv < 5 * gridDim.x;
+}
+
+// Up to 32 sequences: their tiles are counted by every warp for itself, lane b holding sequence b.
+struct Few {
+  int s0, n, kv, nt, incl;
+  __device__ __forceinline__ int load(const KernelArgs& a, int lane, bool tell) {    // returns the number of tiles
+    const int size = 2 * a.tokens;
+    s0 = n = kv = nt = 0;
+    if (lane < a.n_seqs) {
+      if (lengths(a, lane, s0, n, kv) && tell) paged_flag(a.g.status, kBadLength);
+      nt = (n + size - 1) / size;
+    }
+    incl = nt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if ((threadIdx.x & 31) >= o) incl += u;
+    }
+    return __shfl_sync(0xffffffffu, incl, 31);
+  }
+  // Tile e of each lane (any number for lanes that have none): all lanes call.
+  __device__ __forceinline__ int tile(const KernelArgs& a, int e, Piece& p) const {
+    int own = 0;                         // sequences whose tiles all lie ahead of e
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1) {
+      const int v = __shfl_sync(0xffffffffu, incl, (own + step - 1) & 31);
+      if (v <= e) own += step;
+    }
+    own = min(own, 31);
+    const int first = __shfl_sync(0xffffffffu, incl - nt, own);
+    const int b0 = __shfl_sync(0xffffffffu, s0, own), bn = __shfl_sync(0xffffffffu, n, own), bkv = __shfl_sync(0xffffffffu, kv, own);
+    tile_piece(a, own, b0, bn, bkv, e - first, p);
+    return e - first;
+  }
+};
+
+// The list for up to 32 tiles, a lane to a tile; by one warp.
+__device__ __forceinline__ WorkList make_short_list(const KernelArgs& a, const Few& few, int n_tiles, int lane) {
+  const PagedGeom& g = a.g;
+  Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
+  WorkList r{n_tiles, 0, 0, false};
+  Piece p;
+  const int t = few.tile(a, min(lane, n_tiles - 1), p);
+  const bool mine = lane < n_tiles;
+  r.all_steps = (unsigned long long)__reduce_add_sync(0xffffffffu, mine ? (unsigned)p.n_steps : 0u) * g.Hkv;
+  r.every = few_rounds(a, n_tiles);
+  Rounds rounds{0, 0, 1};
+  const int n_max = __reduce_max_sync(0xffffffffu, mine ? p.n_steps : 0);
+  const bool is_full = r.every && mine && Rounds::is_full(p.n_steps, n_max);
+  const unsigned full = __ballot_sync(0xffffffffu, is_full);
+  rounds.plan(a, __popc(full));
+  const int rows = p.n_tok * g.G;
+  int k = mine ? rounds.chunks(a, is_full ? __popc(full & ((1u << lane) - 1u)) : -1, p.n_steps, rows, r.all_steps) : 0;
+  if (a.n_seqs == 1 && !__any_sync(0xffffffffu, k > 1)) {       // the tiles of one sequence are in order
+    r.every = false;
+    r.all_steps = ~0ull;                 // (none is heavy)
+    return r;
+  }
+  const bool is = mine && r.listed(p.n_steps);
+  const int len = is ? (p.n_steps + k - 1) / k : 0;
+  if (!is) k = 0;
+  const int part_rows = k > 1 ? k * g.Hkv * rows : 0;
+  int rank = 0, pieces = 0, rows_at = a.partial ? g.n_tokens * g.Hq : 0, cut_ahead = 0;
+  for (int j = 0; j < n_tiles; ++j) {
+    const int lj = __shfl_sync(0xffffffffu, len, j), kj = __shfl_sync(0xffffffffu, k, j), rj = __shfl_sync(0xffffffffu, part_rows, j);
+    if (lj > len || (lj == len && j < lane)) {
+      rank += kj > 0;
+      pieces += kj;
+      rows_at += rj;
+      cut_ahead += kj > 1;
+    }
+  }
+  if (is) heavy[rank] = Heavy{p.seq, t, k, len, pieces, rows_at, 2 * g.Hkv * cut_ahead, 0};
+  r.n_heavy_pieces = __reduce_add_sync(0xffffffffu, (unsigned)k);
+  __syncwarp();
+  return r;
+}
+
+// The list of all tiles, a thread to a tile (at most kMaxHeavy), of up to 32 sequences; by all threads of the CTA.  Each ranks its own
+// tile over all others: the block meets three times.  The number of pieces is left at the scratch's first integer.
+__device__ __noinline__ void make_middle_list(const KernelArgs& a, const Few few, int n_tiles, unsigned char* scratch, int tid) {
+  const PagedGeom& g = a.g;
+  constexpr int kWarps = (kMaxHeavy + 31) / 32;
+  int* const result = reinterpret_cast<int*>(scratch);
+  int4* const of_warp = reinterpret_cast<int4*>(scratch) + 1;         // [kWarps] {steps, most steps, full tiles, -}
+  int4* const cuts = of_warp + kWarps;                                // [n_tiles] {steps of a chunk, chunks, partial rows, -}
+  const int warp = tid >> 5, lane = tid & 31, n_warps = (n_tiles + 31) >> 5;
+  if (warp >= n_warps) {             // warps without a tile
+    __syncthreads();
+    __syncthreads();
+    __syncthreads();
+    return;
+  }
+  Piece p;
+  const int t = few.tile(a, min(tid, n_tiles - 1), p), rows = p.n_tok * g.G;
+  const bool mine = tid < n_tiles;
+  const unsigned sum = __reduce_add_sync(0xffffffffu, mine ? (unsigned)p.n_steps : 0u);      // (of 32 tiles below 2^23 steps)
+  const int most = __reduce_max_sync(0xffffffffu, mine ? p.n_steps : 0);
+  if (lane == 0) of_warp[warp] = make_int4((int)sum, most, 0, 0);
+  __syncthreads();
+  unsigned long long all = 0;
+  int n_max = 0;
+  for (int w = 0; w < n_warps; ++w) { all += (unsigned)of_warp[w].x; n_max = max(n_max, of_warp[w].y); }
+  all *= g.Hkv;
+  const bool is_full = mine && Rounds::is_full(p.n_steps, n_max);
+  const unsigned m = __ballot_sync(0xffffffffu, is_full);
+  if (lane == 0) of_warp[warp].z = __popc(m);
+  __syncthreads();
+  int full = 0, at = __popc(m & ((1u << lane) - 1u));
+  for (int w = 0; w < n_warps; ++w) {
+    const int f = of_warp[w].z;
+    full += f;
+    at += w < warp ? f : 0;
+  }
+  Rounds rounds;
+  rounds.plan(a, full);
+  const int k = rounds.chunks(a, is_full ? at : -1, p.n_steps, rows, all), len = (p.n_steps + k - 1) / k;
+  if (mine) cuts[tid] = make_int4(len, k, k > 1 ? k * g.Hkv * rows : 0, 0);
+  __syncthreads();
+  int rank = 0, pieces = 0, rows_at = a.partial ? g.n_tokens * g.Hq : 0, cut_ahead = 0, all_pieces = 0;
+#pragma unroll 8
+  for (int j = 0; j < n_tiles; ++j) {
+    const int4 c = cuts[j];
+    const bool ahead = c.x > len || (c.x == len && j < tid);
+    all_pieces += c.y;
+    rank += ahead;
+    pieces += ahead ? c.y : 0;
+    rows_at += ahead ? c.z : 0;
+    cut_ahead += ahead && c.y > 1;
+  }
+  if (mine) (a.heavy + (size_t)blockIdx.x * kMaxHeavy)[rank] = Heavy{p.seq, t, k, len, pieces, rows_at, 2 * g.Hkv * cut_ahead, 0};
+  if (tid == 0) *result = all_pieces;
+}
+
+__device__ __noinline__ WorkList make_list(const KernelArgs& a, const Few& few, int few_tiles, unsigned char* scratch, int tid) {
   const PagedGeom& g = a.g;
   constexpr int kN = kThreads, kWarps = kN / 32;
   const int lane = tid & 31, warp = tid >> 5;
@@ -206,8 +354,10 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* s
     }
     return before + incl - v;
   };
-  WorkList r{0, 0, 0, 0x7fffffff, 1};
-  for (int base = 0; base < a.n_seqs; base += kN) {
+  WorkList r{0, 0, 0, false};
+  const bool is_few = a.n_seqs <= 32;
+  if (is_few) r.n_tiles = few_tiles;
+  for (int base = 0; !is_few && base < a.n_seqs; base += kN) {
     const int b = base + tid;
     int nt = 0, all;
     if (b < a.n_seqs) {
@@ -219,9 +369,12 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* s
     if (b < a.n_seqs) tb[b] = r.n_tiles + before;
     r.n_tiles += all;
   }
-  if (tid == 0) tb[a.n_seqs] = r.n_tiles;
-  __syncthreads();
-  auto tile_of = [&](int e, Piece& p) {
+  if (!is_few) {
+    if (tid == 0) tb[a.n_seqs] = r.n_tiles;
+    __syncthreads();
+  }
+  auto tile_of = [&](int e, Piece& p) {      // all lanes of a warp call; returns the tile's place in its sequence
+    if (is_few) return few.tile(a, e, p);
     int lo = 0, hi = a.n_seqs;             // tb[lo] <= e < tb[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -230,14 +383,16 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* s
     int s0, n, kv;
     lengths(a, lo, s0, n, kv);
     tile_piece(a, lo, s0, n, kv, e - tb[lo], p);
+    return e - tb[lo];
   };
   unsigned long long steps = 0;
   int my_steps = 0;             // of tile tid
-  for (int e = tid; e < r.n_tiles; e += kN) {
+  for (int base = 0; base < r.n_tiles; base += kN) {
+    const int e = base + tid;
     Piece p;
-    tile_of(e, p);
-    steps += (unsigned)p.n_steps;
-    if (e == tid) my_steps = p.n_steps;
+    tile_of(min(e, r.n_tiles - 1), p);
+    if (e < r.n_tiles) steps += (unsigned)p.n_steps;
+    if (base == 0) my_steps = p.n_steps;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
@@ -249,27 +404,16 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* s
   for (int w = 0; w < kWarps; ++w) steps += wide[w];
   __syncthreads();
   r.all_steps = steps * (unsigned long long)g.Hkv;
-  const long long all_pieces = (long long)r.n_tiles * g.Hkv;
-  if (!a.partial && all_pieces > gridDim.x && all_pieces < 5 * gridDim.x) {
-    const int left = (int)(all_pieces % gridDim.x), n_tail = (left + g.Hkv - 1) / g.Hkv;
-    if (left > 0 && 2 * n_tail * g.Hkv <= gridDim.x) {
-      r.tail_from = r.n_tiles - n_tail;
-      r.tail_chunks = (int)gridDim.x / (n_tail * g.Hkv);
-    }
-  }
   // heavy tiles, in the order of the tiles
   int n_heavy = 0;
   for (int base = 0; base < r.n_tiles; base += kN) {
     const int e = base + tid;
-    bool is = false;
-    if (e < r.n_tiles) {
-      if (base) {
-        Piece p;
-        tile_of(e, p);
-        my_steps = p.n_steps;
-      }
-      is = r.listed(a, e, my_steps);
+    if (base) {
+      Piece p;
+      tile_of(min(e, r.n_tiles - 1), p);
+      my_steps = p.n_steps;
     }
+    const bool is = e < r.n_tiles && is_heavy(my_steps, r.all_steps);
     int all;
     const int i = n_heavy + scan(is ? 1 : 0, all);
     if (is && i < kMaxHeavy) found[i] = make_int2(e, 0);
@@ -279,27 +423,25 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, unsigned char* s
   if (n_heavy == 0) return r;
   // ... the heaviest first
   __syncthreads();
-  for (int i = tid; i < n_heavy; i += kN) {
-    Piece p;
-    tile_of(found[i].x, p);
-    const int k = r.chunks(a, found[i].x, p.n_steps, p.n_tok * g.G);
-    found[i].y = (p.n_steps + k - 1) / k;
-  }
+  static_assert(kMaxHeavy <= kN, "a thread to a tile of the list");
+  Piece p;
+  const bool mine = tid < n_heavy;
+  const int e = found[min(tid, n_heavy - 1)].x;
+  const int t = tile_of(e, p);
+  const int k = chunks_of(a, p.n_steps, p.n_tok * g.G, r.all_steps), len = (p.n_steps + k - 1) / k;
+  if (mine) found[tid].y = len;
   __syncthreads();
-  for (int i = tid; i < n_heavy; i += kN) {
-    Piece p;
-    tile_of(found[i].x, p);
-    const int len = found[i].y, k = (p.n_steps + len - 1) / len;
-    int rank = i;
+  if (mine) {
+    int rank = tid;
     if (a.n_seqs > 1) {                // (one sequence's are in order)
       rank = 0;
       for (int j = 0; j < n_heavy; ++j) {
         const int l = found[j].y;
-        rank += l > len || (l == len && j < i);
+        rank += l > len || (l == len && j < tid);
       }
     }
     order[rank] = make_int2(k, p.n_tok * g.G);
-    heavy[rank] = Heavy{p.seq, found[i].x - tb[p.seq], k, len, 0, 0, 0, 0};
+    heavy[rank] = Heavy{p.seq, t, k, len, 0, 0, 0, 0};
   }
   __syncthreads();
   int pieces = 0, rows = a.partial ? g.n_tokens * g.Hq : 0, counters = 0;
@@ -369,12 +511,29 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 
   // ---- the list of work, the same in every CTA; only the producer needs it
   const int size = 2 * R;
-  const WorkList work = make_list(a, smem_al + 2 * kTileBytes, tid);
+  WorkList work{};
+  bool is_short = false;
+  Few few{};
+  int few_tiles = 0;
+  if (a.n_seqs <= 32) {
+    few_tiles = few.load(a, lane, blockIdx.x == 0 && warp == 0);
+    is_short = few_tiles <= 32;
+    if (is_short && warp == kProducerWarp && few_tiles > 0) work = make_short_list(a, few, few_tiles, lane);
+  }
+  if (!is_short && a.n_seqs <= 32 && few_rounds(a, few_tiles)) {
+    make_middle_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
+    work = WorkList{few_tiles, -1, 0, true};
+  } else if (!is_short) {
+    work = make_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
+  }
   if (a.partial)      // tokens of no group have no partial rows
     for (int t = blockIdx.x * kThreads + tid; t < g.n_tokens; t += gridDim.x * kThreads)
       if (t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs)) a.token_parts[t] = PagedToken{0, 0, 0, 0};
-  fence_proxy_async_smem();    // the ring's copies come after what was written there
-  __syncthreads();
+  if (!is_short) {
+    fence_proxy_async_smem();    // the ring's copies come after what was written there
+    __syncthreads();
+    if (work.every) work.n_heavy_pieces = *reinterpret_cast<const int*>(smem_al + 2 * kTileBytes);   // (read by the producer ahead of them)
+  }
 
   // The next piece of work; false: there is none, or a wait has run out.
   uint32_t n_taken = 0;
@@ -403,7 +562,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     int slot = 0;
     uint32_t ph = 1;                         // parity of a slot's emptiness
     const Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
-    const long long heavy_work = (long long)work.n_heavy_pieces * g.Hkv, total = heavy_work + (long long)work.n_tiles * g.Hkv;
+    const long long heavy_work = (long long)work.n_heavy_pieces * g.Hkv, total = heavy_work + (work.every ? 0 : (long long)work.n_tiles * g.Hkv);
     long long w = blockIdx.x;
     int at_heavy = 0;
     int strip = -32, strip_first = 0, strip_all = 0, incl = 0, nt = 0, s0 = 0, n = 0, kv = 0;   // 32 sequences, one a lane
@@ -464,7 +623,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const int h = p.head, t = e - strip_first - __shfl_sync(0xffffffffu, incl - nt, own);
           tile_piece(a, strip + own, __shfl_sync(0xffffffffu, s0, own), __shfl_sync(0xffffffffu, n, own), __shfl_sync(0xffffffffu, kv, own), t, p);
           p.head = h;
-          if (work.listed(a, e, p.n_steps)) {     // it was among those
+          if (work.listed(p.n_steps)) {     // it was among those
             w = __shfl_sync(0xffffffffu, next, 0);
             continue;
           }
@@ -873,36 +1032,59 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       if (*reinterpret_cast<volatile int*>(&tail.last[s])) {
         const int n_rows = min(R, n_tok - s * R) * g.G, n_chunks = it.n_chunks, step = it.part_step;
         const size_t first_row = part_at - (size_t)(it.step0 / it.chunk_steps) * step + s * R * g.G;
-        constexpr int kRows = 4;                         // of a warp at a time, so that their loads are in flight together
-        for (int r0 = warp & 7; r0 < n_rows; r0 += 8 * kRows) {
-          Partial p[kRows];
+        // four rows of a warp at a time: first their chunks' weights, a lane to a row and chunk, then the sums, whose loads wait for nothing
+        for (int r0 = (warp & 7) * 4; r0 < n_rows; r0 += 32) {
+          const float* const src = a.parts + (first_row + r0) * kPagedPartStride;
+          const size_t chunk_at = (size_t)step * kPagedPartStride;
+          const int my_row = lane >> 3;
+          const bool there = r0 + my_row < n_rows;
+          float top = -INFINITY, sum = 0.f;
+          for (int c0 = 0; c0 < n_chunks; c0 += 8) {
+            const int c = c0 + (lane & 7);
+            const float2 ml = there && c < n_chunks ? __ldcg(reinterpret_cast<const float2*>(src + c * chunk_at + my_row * kPagedPartStride + kD))
+                                                    : make_float2(-INFINITY, 0.f);
+            float m = ml.x;
 #pragma unroll
-          for (int k = 0; k < kRows; ++k) p[k].clear();
-          const float* src = a.parts + (first_row + r0) * kPagedPartStride;
-          for (int c = 0; c < n_chunks; ++c, src += (size_t)step * kPagedPartStride) {
-            float4 o[kRows];
-            float2 ml[kRows];
+            for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            m = fmaxf(m, top);
+            const float at = m == -INFINITY ? 0.f : m;
+            float l_sum = ml.y * ex2_approx(ml.x - at);
 #pragma unroll
-            for (int k = 0; k < kRows; ++k) {
-              const float* x = src + (r0 + 8 * k < n_rows ? 8 * k : 0) * kPagedPartStride;
-              o[k] = __ldcg(reinterpret_cast<const float4*>(x) + lane);
-              ml[k] = __ldcg(reinterpret_cast<const float2*>(x + kD));
+            for (int o = 1; o < 8; o <<= 1) l_sum += __shfl_xor_sync(0xffffffffu, l_sum, o);
+            sum = sum * ex2_approx(top - at) + l_sum;
+            top = m;
+          }
+          const float at = top == -INFINITY ? 0.f : top, f_row = sum == 0.f ? 0.f : 1.f / sum;
+          float4 acc[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c0 = 0; c0 < n_chunks; c0 += 8) {
+            const int c = c0 + (lane & 7);
+            const float m = there && c < n_chunks ? __ldcg(src + c * chunk_at + my_row * kPagedPartStride + kD) : -INFINITY;
+            const float weight = ex2_approx(m - at) * f_row;
+            const int n_c = min(8, n_chunks - c0);
+#pragma unroll 4
+            for (int i = 0; i < n_c; ++i) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float w = __shfl_sync(0xffffffffu, weight, k * 8 + i);
+                const float* x = src + (c0 + i) * chunk_at + (r0 + k < n_rows ? k : 0) * kPagedPartStride;
+                const float4 o = __ldcg(reinterpret_cast<const float4*>(x) + lane);
+                acc[k].x = fmaf(o.x, w, acc[k].x); acc[k].y = fmaf(o.y, w, acc[k].y);
+                acc[k].z = fmaf(o.z, w, acc[k].z); acc[k].w = fmaf(o.w, w, acc[k].w);
+              }
             }
-#pragma unroll
-            for (int k = 0; k < kRows; ++k) p[k].join(ml[k].x, ml[k].y, o[k]);
           }
 #pragma unroll
-          for (int k = 0; k < kRows; ++k) {
-            const int row = r0 + 8 * k;
-            if (row >= n_rows) break;
+          for (int k = 0; k < 4; ++k) {
+            const int row = r0 + k;
+            const float lse = __shfl_sync(0xffffffffu, sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2, k * 8);
+            if (row >= n_rows) continue;
             const int i = s * R + (row * a.g_inv >> 16), hd = row - (row * a.g_inv >> 16) * g.G;
-            const float f = p[k].l == 0.f ? 0.f : 1.f / p[k].l;
-            uint2 v;
-            v.x = pack16<kF16>(p[k].o[0] * f, p[k].o[1] * f);
-            v.y = pack16<kF16>(p[k].o[2] * f, p[k].o[3] * f);
             const size_t out_row = head_row + (uint32_t)(i * g.Hq + hd);
-            reinterpret_cast<uint2*>(a.out)[out_row * (kD / 4) + lane] = v;
-            if (a.lse && lane == 0) a.lse[out_row] = p[k].l == 0.f ? -INFINITY : (p[k].m + __log2f(p[k].l)) * kLn2;
+            reinterpret_cast<uint2*>(a.out)[out_row * (kD / 4) + lane] =
+                make_uint2(pack16<kF16>(acc[k].x, acc[k].y), pack16<kF16>(acc[k].z, acc[k].w));
+            if (a.lse && lane == 0) a.lse[out_row] = lse;
           }
         }
       }
