@@ -37,7 +37,7 @@ constexpr int kThreads = 640;
 constexpr int kSlots = 5;                         // K and V tiles in one ring, in the order in which they are used
 constexpr int kTileBytes = kKvTileBytes;          // 32 KB
 constexpr uint32_t kColO = 256;
-constexpr int kMaxHeavy = 2 * kSms + kSms / 2;    // tiles of at least half an SM's mean share, and those of a ragged last round
+constexpr int kMaxHeavy = 2 * kSms;               // tiles of at least half an SM's mean share
 constexpr int kItemReaders = kSoftmaxWarps + 2;   // warps that take a piece from the producer
 
 // A piece of work: a tile of rows of one kv head against a range of steps.
@@ -157,40 +157,12 @@ __device__ __forceinline__ void terms(const uint32_t (&x)[32], f32x2 scale2, flo
   }
 }
 
-// The list of work: heavy tiles, or all of them where they make few rounds, in falling order of their chunks, at a.heavy; made by all threads of
-// the CTA in `scratch`, or for a few tiles by one warp.
+// The list of work: heavy tiles, in falling order of their chunks, at a.heavy; made by all threads of the CTA in `scratch`, or for a few
+// tiles by one warp.
 struct WorkList {
   int n_tiles, n_heavy_pieces;
   unsigned long long all_steps;    // of all tiles and heads
-  bool every;                      // the list has all tiles
-  __device__ __forceinline__ bool listed(int n) const { return every || is_heavy(n, all_steps); }
 };
-
-// Few rounds of pieces (less than five, of tiles that fit the list) are all listed, so that they are dealt from the heaviest down, and those of them that
-// would begin a ragged last round are cut to fill it: of the tiles of at least 0.6 of the largest one's steps, those beyond whole
-// rounds, the last ones.  (312 pieces of 14 steps on 148 SMs: 102 us uncut.)
-struct Rounds {
-  int n_full, n_tail, tail_chunks;
-  __device__ __forceinline__ static bool is_full(int n, int n_max) { return 10 * n >= 6 * n_max; }
-  __device__ __forceinline__ void plan(const KernelArgs& a, int full) {
-    n_full = full;
-    n_tail = 0;
-    tail_chunks = 1;
-    const int left = full * a.g.Hkv % (int)gridDim.x, tail = (left + a.g.Hkv - 1) / a.g.Hkv;
-    if (a.partial || full * a.g.Hkv <= (int)gridDim.x || left == 0 || 2 * tail * a.g.Hkv > (int)gridDim.x) return;
-    n_tail = tail;
-    tail_chunks = (int)gridDim.x / (tail * a.g.Hkv);
-  }
-  // chunks of a tile that is number `at` of the full ones, or (-1) none of them
-  __device__ __forceinline__ int chunks(const KernelArgs& a, int at, int n, int rows, unsigned long long all) const {
-    if (at < n_full - n_tail) return chunks_of(a, n, rows, all);
-    const int k = max(1, min(min(tail_chunks, n / 3), (int)sqrtf(375.f * n / rows))), len = (n + k - 1) / k;
-    return (n + len - 1) / len;
-  }
-};
-__device__ __forceinline__ bool few_rounds(const KernelArgs& a, int n_tiles) {
-  return n_tiles <= kMaxHeavy && (long long)n_tiles * a.g.Hkv < 5 * gridDim.x;
-}
 
 // Up to 32 sequences: their tiles are counted by every warp for itself, lane b holding sequence b.
 struct Few {
@@ -230,25 +202,18 @@ struct Few {
 __device__ __forceinline__ WorkList make_short_list(const KernelArgs& a, const Few& few, int n_tiles, int lane) {
   const PagedGeom& g = a.g;
   Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
-  WorkList r{n_tiles, 0, 0, false};
+  WorkList r{n_tiles, 0, 0};
   Piece p;
   const int t = few.tile(a, min(lane, n_tiles - 1), p);
   const bool mine = lane < n_tiles;
-  r.all_steps = (unsigned long long)__reduce_add_sync(0xffffffffu, mine ? (unsigned)p.n_steps : 0u) * g.Hkv;
-  r.every = few_rounds(a, n_tiles);
-  Rounds rounds{0, 0, 1};
-  const int n_max = __reduce_max_sync(0xffffffffu, mine ? p.n_steps : 0);
-  const bool is_full = r.every && mine && Rounds::is_full(p.n_steps, n_max);
-  const unsigned full = __ballot_sync(0xffffffffu, is_full);
-  rounds.plan(a, __popc(full));
+  r.all_steps = (unsigned long long)__reduce_add_sync(0xffffffffu, mine ? (unsigned)p.n_steps : 0u) * g.Hkv;   // (32 tiles of less than 2^23 steps)
   const int rows = p.n_tok * g.G;
-  int k = mine ? rounds.chunks(a, is_full ? __popc(full & ((1u << lane) - 1u)) : -1, p.n_steps, rows, r.all_steps) : 0;
+  int k = mine ? chunks_of(a, p.n_steps, rows, r.all_steps) : 0;
   if (a.n_seqs == 1 && !__any_sync(0xffffffffu, k > 1)) {       // the tiles of one sequence are in order
-    r.every = false;
     r.all_steps = ~0ull;                 // (none is heavy)
     return r;
   }
-  const bool is = mine && r.listed(p.n_steps);
+  const bool is = mine && is_heavy(p.n_steps, r.all_steps);
   const int len = is ? (p.n_steps + k - 1) / k : 0;
   if (!is) k = 0;
   const int part_rows = k > 1 ? k * g.Hkv * rows : 0;
@@ -266,62 +231,6 @@ __device__ __forceinline__ WorkList make_short_list(const KernelArgs& a, const F
   r.n_heavy_pieces = __reduce_add_sync(0xffffffffu, (unsigned)k);
   __syncwarp();
   return r;
-}
-
-// The list of all tiles, a thread to a tile (at most kMaxHeavy), of up to 32 sequences; by all threads of the CTA.  Each ranks its own
-// tile over all others: the block meets three times.  The number of pieces is left at the scratch's first integer.
-__device__ __noinline__ void make_middle_list(const KernelArgs& a, const Few few, int n_tiles, unsigned char* scratch, int tid) {
-  const PagedGeom& g = a.g;
-  constexpr int kWarps = (kMaxHeavy + 31) / 32;
-  int* const result = reinterpret_cast<int*>(scratch);
-  int4* const of_warp = reinterpret_cast<int4*>(scratch) + 1;         // [kWarps] {steps, most steps, full tiles, -}
-  int4* const cuts = of_warp + kWarps;                                // [n_tiles] {steps of a chunk, chunks, partial rows, -}
-  const int warp = tid >> 5, lane = tid & 31, n_warps = (n_tiles + 31) >> 5;
-  if (warp >= n_warps) {             // warps without a tile
-    __syncthreads();
-    __syncthreads();
-    __syncthreads();
-    return;
-  }
-  Piece p;
-  const int t = few.tile(a, min(tid, n_tiles - 1), p), rows = p.n_tok * g.G;
-  const bool mine = tid < n_tiles;
-  const unsigned sum = __reduce_add_sync(0xffffffffu, mine ? (unsigned)p.n_steps : 0u);      // (of 32 tiles below 2^23 steps)
-  const int most = __reduce_max_sync(0xffffffffu, mine ? p.n_steps : 0);
-  if (lane == 0) of_warp[warp] = make_int4((int)sum, most, 0, 0);
-  __syncthreads();
-  unsigned long long all = 0;
-  int n_max = 0;
-  for (int w = 0; w < n_warps; ++w) { all += (unsigned)of_warp[w].x; n_max = max(n_max, of_warp[w].y); }
-  all *= g.Hkv;
-  const bool is_full = mine && Rounds::is_full(p.n_steps, n_max);
-  const unsigned m = __ballot_sync(0xffffffffu, is_full);
-  if (lane == 0) of_warp[warp].z = __popc(m);
-  __syncthreads();
-  int full = 0, at = __popc(m & ((1u << lane) - 1u));
-  for (int w = 0; w < n_warps; ++w) {
-    const int f = of_warp[w].z;
-    full += f;
-    at += w < warp ? f : 0;
-  }
-  Rounds rounds;
-  rounds.plan(a, full);
-  const int k = rounds.chunks(a, is_full ? at : -1, p.n_steps, rows, all), len = (p.n_steps + k - 1) / k;
-  if (mine) cuts[tid] = make_int4(len, k, k > 1 ? k * g.Hkv * rows : 0, 0);
-  __syncthreads();
-  int rank = 0, pieces = 0, rows_at = a.partial ? g.n_tokens * g.Hq : 0, cut_ahead = 0, all_pieces = 0;
-#pragma unroll 8
-  for (int j = 0; j < n_tiles; ++j) {
-    const int4 c = cuts[j];
-    const bool ahead = c.x > len || (c.x == len && j < tid);
-    all_pieces += c.y;
-    rank += ahead;
-    pieces += ahead ? c.y : 0;
-    rows_at += ahead ? c.z : 0;
-    cut_ahead += ahead && c.y > 1;
-  }
-  if (mine) (a.heavy + (size_t)blockIdx.x * kMaxHeavy)[rank] = Heavy{p.seq, t, k, len, pieces, rows_at, 2 * g.Hkv * cut_ahead, 0};
-  if (tid == 0) *result = all_pieces;
 }
 
 __device__ __noinline__ WorkList make_list(const KernelArgs& a, const Few& few, int few_tiles, unsigned char* scratch, int tid) {
@@ -354,7 +263,7 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, const Few& few, 
     }
     return before + incl - v;
   };
-  WorkList r{0, 0, 0, false};
+  WorkList r{0, 0, 0};
   const bool is_few = a.n_seqs <= 32;
   if (is_few) r.n_tiles = few_tiles;
   for (int base = 0; !is_few && base < a.n_seqs; base += kN) {
@@ -520,19 +429,13 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     is_short = few_tiles <= 32;
     if (is_short && warp == kProducerWarp && few_tiles > 0) work = make_short_list(a, few, few_tiles, lane);
   }
-  if (!is_short && a.n_seqs <= 32 && few_rounds(a, few_tiles)) {
-    make_middle_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
-    work = WorkList{few_tiles, -1, 0, true};
-  } else if (!is_short) {
-    work = make_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
-  }
+  if (!is_short) work = make_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
   if (a.partial)      // tokens of no group have no partial rows
     for (int t = blockIdx.x * kThreads + tid; t < g.n_tokens; t += gridDim.x * kThreads)
       if (t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs)) a.token_parts[t] = PagedToken{0, 0, 0, 0};
   if (!is_short) {
     fence_proxy_async_smem();    // the ring's copies come after what was written there
     __syncthreads();
-    if (work.every) work.n_heavy_pieces = *reinterpret_cast<const int*>(smem_al + 2 * kTileBytes);   // (read by the producer ahead of them)
   }
 
   // The next piece of work; false: there is none, or a wait has run out.
@@ -562,7 +465,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     int slot = 0;
     uint32_t ph = 1;                         // parity of a slot's emptiness
     const Heavy* const heavy = a.heavy + (size_t)blockIdx.x * kMaxHeavy;
-    const long long heavy_work = (long long)work.n_heavy_pieces * g.Hkv, total = heavy_work + (work.every ? 0 : (long long)work.n_tiles * g.Hkv);
+    const long long heavy_work = (long long)work.n_heavy_pieces * g.Hkv, total = heavy_work + (long long)work.n_tiles * g.Hkv;
     long long w = blockIdx.x;
     int at_heavy = 0;
     int strip = -32, strip_first = 0, strip_all = 0, incl = 0, nt = 0, s0 = 0, n = 0, kv = 0;   // 32 sequences, one a lane
@@ -623,7 +526,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const int h = p.head, t = e - strip_first - __shfl_sync(0xffffffffu, incl - nt, own);
           tile_piece(a, strip + own, __shfl_sync(0xffffffffu, s0, own), __shfl_sync(0xffffffffu, n, own), __shfl_sync(0xffffffffu, kv, own), t, p);
           p.head = h;
-          if (work.listed(p.n_steps)) {     // it was among those
+          if (is_heavy(p.n_steps, work.all_steps)) {     // it was among those
             w = __shfl_sync(0xffffffffu, next, 0);
             continue;
           }
@@ -1152,9 +1055,8 @@ bool paged_kv_map(CUtensorMap* out, const void* base, const PagedGeom& g, int ro
 PagedWs paged_ws(int B, int Hq, int Hkv, int n_tokens, int n_groups) {
   PagedWs w{};
   const int G = Hq / Hkv;
-  // chunks of cut tiles are no more than the SMs, and as many again of a ragged last round; with a shared prefix every token has rows of its
-  // own in any case
-  w.max_rows = 2ll * kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)n_tokens * Hq : 0);
+  // chunks of cut tiles are no more than the SMs; with a shared prefix every token has rows of its own in any case
+  w.max_rows = (long long)kSms * std::min((long long)kPagedRows, (long long)n_tokens * G) + (n_groups ? (long long)n_tokens * Hq : 0);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t off = kPagedPlan;
   w.sched = off;  off = up(off + (16 + 2 * kSms) * 4);
