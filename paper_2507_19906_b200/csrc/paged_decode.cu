@@ -31,7 +31,8 @@ constexpr int kCtas = 2 * kSms;                        // two to an SM
 constexpr int kPartBytes = kSlotRows * kRowBytes;      // K or V of a slot: 16 KB
 constexpr int kSlotBytes = 2 * kPartBytes;
 constexpr int kStride = kPagedPartStride;              // floats of a warp's partial row: heads land in distinct banks
-constexpr int kUnitCost = 1;                           // what a unit costs beside its rows, in blocks
+constexpr int kUnitCost = 2;                           // what a unit costs beside its rows, in blocks (with 1, 2, 3: 768 short units and a prefix 78, 73, 73 us,
+                                                       // 64 of them 27.5, 26.0, 27.7, 256 long ones 140, 141, 140)
 constexpr int kMinShare = 2;                           // of a CTA's part of the line: at least one block of a unit
 // What is in shared memory behind the ring.
 struct Tail {

@@ -208,6 +208,12 @@ PREFILLS = [
     ([150], [3000], 16, 2, 128, 700, 130, BF, 0),
     ([1, 1, 1, 1], [50, 600, 1000, 1], 32, 8, 64, 256, 32, BF, 0),
     ([1000], [1100], 4, 4, 64, 128, 128, FP, 0),
+    # more tiles of rows than a warp lists, some of them cut along the keys
+    ([3000], [3000], 8, 2, 64, 0, 0, BF, 0),
+    # more sequences than a warp counts, some with most of the work
+    ([1, 0, 3, 40] * 12 + [300, 130], [5, 0, 700, 40] * 12 + [2500, 130], 8, 2, 16, 0, 0, FP, 1),
+    # more sequences than a CTA has threads
+    ([1] * 650 + [70], [1 + i % 130 for i in range(650)] + [1500], 4, 1, 16, 90, 4, BF, 0),
 ]
 
 
@@ -250,6 +256,8 @@ PREFIXES = [
     ([2, 1, 4, 3], [64, 2000, 129], 40, 16, 2, 128, FP),
     ([33, 0], [4000], 0, 40, 8, 256, BF),
     ([0, 9, 2], [100, 700], 130, 5, 1, 16, BF),
+    # more groups than a warp counts, one with most of the rows
+    ([2, 1, 0, 3] * 10 + [1], [17 * i % 200 for i in range(39)] + [3000], 10, 8, 2, 32, BF),
 ]
 
 
@@ -276,6 +284,57 @@ def test_prefix_decode(cuda_lib, case):
         cd.calidrop_paged_prefix_decode(p, q, both.K, both.V, i32(borders), prefix_table, i32(plens), table, i32(kv), r.out, r.lse, ws)
         assert status_of(ws) == 0
         check_prefill(both, r, q, [1] * B, kv, Hq=Hq, prefix=prefix)
+
+
+def test_no_tokens(cuda_lib):
+    pool = Pool([100], Hkv=2, page=64)
+    p = cd.make_paged_params(B=1, Hq=8, Hkv=2, page_size=64, n_pages=pool.n_pages, max_pages=pool.max_pages)
+    ws = workspace(p, 0)
+    q = torch.empty((0, 8, D), dtype=BF, device="cuda")
+    k = torch.empty((0, 2, D), dtype=BF, device="cuda")
+    z = i32([0, 0])
+    n = cd.calidrop_launch_count()
+    cd.calidrop_paged_prefill(p, q, pool.K, pool.V, pool.table, z, i32([100]), q, None, ws)
+    cd.calidrop_paged_append(p, q, k, k, None, None, pool.K, pool.V, pool.table, z, i32([100]), q, ws)
+    assert cd.calidrop_launch_count() == n and status_of(ws) == 0
+    # tokens that are all padding
+    q = queries(5, 8, BF, 1)
+    r = run_prefill(pool, q, [0], [100], Hq=8)
+    check_prefill(pool, r, q, [0], [100], Hq=8)
+
+
+def test_calls_at_once(cuda_lib):
+    """Two streams with a workspace each, over the same cache; and calls of every kind in turn in one workspace."""
+    kv = [900, 30, 2000]
+    pool = Pool(kv, Hkv=2, page=32, seed=3)
+    q = queries(3 + 200, 8, BF, 4)
+    p = cd.make_paged_params(B=3, Hq=8, Hkv=2, page_size=32, n_pages=pool.n_pages, max_pages=pool.max_pages, n_groups=1,
+                             max_prefix_pages=pool.max_pages)
+    lens, new = i32(kv), [100, 3, 100]
+    st = starts(new)
+    out = {}
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for round_ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                if round_ == 0:
+                    out[i] = dict(ws=workspace(p, 203), o=[torch.empty_like(q) for _ in range(3)], l=[torch.empty((203, 8), device="cuda") for _ in range(3)])
+                w = out[i]
+                cd.calidrop_paged_prefill(p, q, pool.K, pool.V, pool.table, st, lens, w["o"][0], w["l"][0], w["ws"])
+                cd.calidrop_paged_decode(p, q[:3], pool.K, pool.V, pool.table, lens, w["o"][1][:3], w["l"][1][:3], w["ws"])
+                cd.calidrop_paged_prefix_decode(p, q[:3], pool.K, pool.V, i32([0, 2]), pool.table[2:], lens[2:], pool.table, lens, w["o"][2][:3],
+                                                w["l"][2][:3], w["ws"])
+    torch.cuda.synchronize()
+    for w in out.values():
+        assert status_of(w["ws"]) == 0
+        r = type("R", (), {})
+        r.out, r.lse = w["o"][0], w["l"][0]
+        check_prefill(pool, r, q, new, kv, Hq=8)
+        r.out, r.lse = w["o"][1][:3], w["l"][1][:3]
+        check_prefill(pool, r, q[:3], [1] * 3, kv, Hq=8)
+        r.out, r.lse = w["o"][2][:3], w["l"][2][:3]
+        check_prefill(pool, r, q[:3], [1] * 3, kv, Hq=8, prefix=[(pool, 2, kv[2]), (pool, 2, kv[2]), None])
 
 
 # ------------------------------------------------------------------------------------------ masked and broken data
