@@ -14,7 +14,8 @@
 // slot, and a slot is consumed by the four warps, 16 rows each, with mma.sync, keys on the 16-row side (as in decode.cu).  The
 // producer runs ahead over the borders of units, so that the memory does not wait for a unit's end, and two CTAs share an SM, so that
 // one streams while the other ends a unit.  (One CTA of eight stream warps and six slots: 768 units of 24 to 600 rows, joined with
-// a shared prefix, 87 us.)
+// a shared prefix, 87 us, now 40.)  32 caches of 600 to 16000 rows, 0.9 GB: 140 us, 98 % of the copy bandwidth; 48 with a window of 4064 rows, 0.66 GB:
+// 108 us, 94 %; one cache of 512 visible rows: 8 us, a chain of lengths, table, rows, partials, ticket and join.
 #include <algorithm>
 
 #include "paged_common.cuh"
@@ -31,8 +32,9 @@ constexpr int kCtas = 2 * kSms;                        // two to an SM
 constexpr int kPartBytes = kSlotRows * kRowBytes;      // K or V of a slot: 16 KB
 constexpr int kSlotBytes = 2 * kPartBytes;
 constexpr int kStride = kPagedPartStride;              // floats of a warp's partial row: heads land in distinct banks
-constexpr int kUnitCost = 2;                           // what a unit costs beside its rows, in blocks (with 1, 2, 3: 768 short units and a prefix 78, 73, 73 us,
-                                                       // 64 of them 27.5, 26.0, 27.7, 256 long ones 140, 141, 140)
+// What a unit costs beside its rows, in blocks.  With 1, 2, 3: 768 short units and their prefix 78, 73, 73 us, 64 of them 27.5, 26.0, 27.7, 256 long units
+// 140, 141, 140.
+constexpr int kUnitCost = 2;
 constexpr int kMinShare = 2;                           // of a CTA's part of the line: at least one block of a unit
 // What is in shared memory behind the ring.
 struct Tail {

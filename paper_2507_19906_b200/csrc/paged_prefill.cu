@@ -13,11 +13,16 @@
 //
 // A CTA works on two streams of 128 rows; while one stream has its softmax the other has the tensor cores.  A stream is two
 // warpgroups, two threads to a row, 64 of a tile's keys each.  Tensor memory: S of the streams at columns 0 and 128, O at 256 and
-// 384.  P, rounded to 16 bits, overwrites S, the first 32 of the 64 columns of each warpgroup.  One warp issues all MMAs of a stream, and
-// those of an issuing thread run in order, so
+// 384.  P, rounded to 16 bits, overwrites S, the first 32 of the 64 columns of each warpgroup.  One warp issues all MMAs, and those of an
+// issuing thread run in order, so
 //   * S(j+1) may be issued behind P V(j), which reads P from the same columns;
 //   * a stream that has been told of S(j) also knows that its P V(j-1) is done, and may rescale O itself.
 // P is handed over in two parts, of 48 keys and 16, so that little of P V is left when the last is done.
+//
+// What bounds it: for long prompts the power limit, behind it the chain of a stream's step (S, its way to the registers, the exponentials, P,
+// P V: 3000 cycles for two streams where the tensor cores need 2048); causal, 32 heads x 8192 tokens take 501 to 511 us from box to box
+// (1.08 PFLOP/s; 567 with a thread to a row, which held 128 logits and worked on few exponentials at a time).  For short prompts the chain of
+// a launch: 6 us of start, list and first loads, and 3 at the end.  For a prefix shared by few rows the memory (64 KB a step and SM in 1.4 us).
 #include <algorithm>
 
 #include "exp2.cuh"
@@ -266,6 +271,7 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, const Few& few, 
   WorkList r{0, 0, 0};
   const bool is_few = a.n_seqs <= 32;
   if (is_few) r.n_tiles = few_tiles;
+  const int most_tiles = g.n_tokens / size + a.n_seqs;     // of starts that do not fall
   for (int base = 0; !is_few && base < a.n_seqs; base += kN) {
     const int b = base + tid;
     int nt = 0, all;
@@ -276,6 +282,7 @@ __device__ __noinline__ WorkList make_list(const KernelArgs& a, const Few& few, 
     }
     const int before = scan(nt, all);
     if (b < a.n_seqs) tb[b] = r.n_tiles + before;
+    if (all > most_tiles - r.n_tiles) return WorkList{0, 0, 0};   // (flagged above; the sums could overflow)
     r.n_tiles += all;
   }
   if (!is_few) {
