@@ -171,11 +171,13 @@ struct Args {
   }
   // No tensor of another device, and none of the host's: its address would mean nothing to the kernels.
   void on_this_device(Py_ssize_t n) {
+    int device = -1;                     // the current one, asked for once
     for (Py_ssize_t i = 1; ok && i < n; ++i) {
       if (!THPVariable_CheckExact(a[i])) continue;
       try {
         const at::Tensor& t = THPVariable_Unpack(a[i]);
-        if (t.is_cuda() && t.get_device() == c10::cuda::current_device()) continue;
+        if (t.is_cuda() && device < 0) device = c10::cuda::current_device();
+        if (t.is_cuda() && t.get_device() == device) continue;
         PyErr_SetString(PyExc_ValueError, "tensors on the current CUDA device expected");
       } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -185,6 +187,13 @@ struct Args {
   }
   // the first dimension of a tensor
   int32_t tokens(int i) {
+    if (ok && THPVariable_CheckExact(a[i])) {
+      try {
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (t.dim() > 0 && t.size(0) == (int32_t)t.size(0)) return (int32_t)t.size(0);
+      } catch (...) {
+      }
+    }
     PyObject* s = ok ? PyObject_GetAttrString(a[i], "shape") : nullptr;
     PyObject* n = s ? PySequence_GetItem(s, 0) : nullptr;
     Py_XDECREF(s);
