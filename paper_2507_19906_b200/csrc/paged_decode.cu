@@ -370,7 +370,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     };
     auto finish = [&](Partial& p, int head) {
       const long long last_row = prefix.x + (long long)(prefix.y - 1) * prefix.z + (long long)h * prefix.w + head;
-      if (prefix.y > 0 && prefix.x >= 0 && prefix.z >= 0 && prefix.w >= 0 && last_row < a.max_rows)   // (not so only after a group_start that falls)
+      // (not so only where groups overlap after a group_start that falls, whose records may be a mixture)
+      if (prefix.y > 0 && prefix.y <= kSms && prefix.x >= 0 && prefix.z >= 0 && prefix.w >= 0 && last_row < a.max_rows)
         join_rows(p, prefix.y, lane, [&](int i) { return a.prefix_rows + ((size_t)prefix.x + (size_t)i * prefix.z + (size_t)h * prefix.w + head) * kStride; });
       const int hq = h * g.G + head;
       const float inv = p.l == 0.f ? 0.f : 1.f / p.l;    // no visible row: zeros

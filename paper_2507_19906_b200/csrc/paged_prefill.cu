@@ -101,13 +101,16 @@ struct KernelArgs {
   float* lse;
 };
 
+// Whether the tokens [s0, s1) are those of a sequence: else it is taken to have none.
+__device__ __forceinline__ bool good_starts(const KernelArgs& a, int s0, int s1) { return s0 >= 0 && s1 >= s0 && s1 <= a.g.n_tokens; }
+
 // Sequence b: its first token, number of tokens and cached rows, held to what the buffers allow.
 __device__ __forceinline__ bool lengths(const KernelArgs& a, int b, int& s0, int& n, int& kv) {
   const int cap = a.g.max_pages << a.g.lg_page;
   s0 = __ldg(a.q_start + b);
   const int s1 = __ldg(a.q_start + b + 1);
   kv = __ldg(a.kv_len + b);
-  const bool bad = s0 < 0 || s1 < s0 || s1 > a.g.n_tokens, bad_kv = kv < 0 || kv > cap;
+  const bool bad = !good_starts(a, s0, s1), bad_kv = kv < 0 || kv > cap;
   n = bad ? 0 : s1 - s0;
   kv = min(max(kv, 0), cap);
   return bad || bad_kv;
@@ -437,9 +440,22 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     if (is_short && warp == kProducerWarp && few_tiles > 0) work = make_short_list(a, few, few_tiles, lane);
   }
   if (!is_short) work = make_list(a, few, few_tiles, smem_al + 2 * kTileBytes, tid);
-  if (a.partial)      // tokens of no group have no partial rows
-    for (int t = blockIdx.x * kThreads + tid; t < g.n_tokens; t += gridDim.x * kThreads)
-      if (t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs)) a.token_parts[t] = PagedToken{0, 0, 0, 0};
+  if (a.partial)      // tokens of no group, or of one that is not taken, have no partial rows; the workspace may hold anything there
+    for (int t0 = blockIdx.x * kThreads + warp * 32; t0 < g.n_tokens; t0 += gridDim.x * kThreads) {
+      bool good = (a.n_seqs <= 32 ? few_tiles : work.n_tiles) > 0;
+      for (int b = lane; b < a.n_seqs; b += 32) good = good && good_starts(a, __ldg(a.q_start + b), __ldg(a.q_start + b + 1));
+      good = __all_sync(0xffffffffu, good);
+      const int t = t0 + lane;
+      if (t >= g.n_tokens) continue;
+      bool none = !good || t < __ldg(a.q_start) || t >= __ldg(a.q_start + a.n_seqs);
+      if (!good && (a.n_seqs <= 32 || work.n_tiles > 0))
+        for (int b = 0; none && b < a.n_seqs; ++b) {
+          int s0, n, kv;
+          lengths(a, b, s0, n, kv);
+          none = t < s0 || t >= s0 + n;
+        }
+      if (none) a.token_parts[t] = PagedToken{0, 0, 0, 0};
+    }
   if (!is_short) {
     fence_proxy_async_smem();    // the ring's copies come after what was written there
     __syncthreads();

@@ -1,0 +1,71 @@
+"""Bad and extreme device data in the operators over a cache in pages: what is flagged, what stays right beside it."""
+import math
+
+import pytest
+import torch
+
+from paper_2507_19906_b200 import binding as cd
+from paged_util import D, Pool, check_prefill, i32, queries, status_of, workspace
+
+pytestmark = pytest.mark.gpu
+
+BF, FP = torch.bfloat16, torch.float16
+
+
+# ------------------------------------------------------------------------------------------ shared prefix
+class Prefixed:
+    """B sequences of a few own rows, and prefixes for `plens` groups, in one pool."""
+
+    def __init__(self, B, plens, own, Hq=8, Hkv=2, page=32, dtype=BF):
+        self.B, self.plens, self.Hq = B, plens, Hq
+        self.kv = [1 + (i * 13) % own for i in range(B)]
+        self.pool = Pool(self.kv + plens, Hkv=Hkv, page=page, dtype=dtype, seed=B)
+        self.table, self.prefix_table = self.pool.table[:B].contiguous(), self.pool.table[B:].contiguous()
+        self.q = queries(B, Hq, dtype, 1)
+        self.p = cd.make_paged_params(B=B, Hq=Hq, Hkv=Hkv, page_size=page, n_pages=self.pool.n_pages, max_pages=self.pool.max_pages, dtype=dtype,
+                                      n_groups=len(plens), max_prefix_pages=self.pool.max_pages)
+        self.ws = workspace(self.p, B)
+        # where a call with groups keeps, for each token, which partial rows are its own: 16 bytes each, behind the parts whose size
+        # depends on nothing
+        none = cd.make_paged_params(B=B, Hq=Hq, Hkv=Hkv, page_size=page, n_pages=self.pool.n_pages, max_pages=self.pool.max_pages, dtype=dtype)
+        at = cd.calidrop_paged_workspace_bytes(none, 0)
+        self.records = self.ws[at:at + 16 * B].view(torch.int32)
+
+    def run(self, borders, plens=None, kv=None):
+        r = type("R", (), {})()
+        r.out = torch.full_like(self.q, 7.0)
+        r.lse = torch.full((self.B, self.Hq), 7.0, device="cuda")
+        cd.calidrop_paged_prefix_decode(self.p, self.q, self.pool.K, self.pool.V, i32(borders), self.prefix_table, i32(plens or self.plens),
+                                        self.table, i32(kv or self.kv), r.out, r.lse, self.ws)
+        r.status = status_of(self.ws)
+        self.ws[:4].zero_()
+        return r
+
+    def check(self, r, b, prefix):
+        """Sequence b, over the prefix of that index (None: its own rows only)."""
+        one = type("R", (), dict(out=r.out[b:b + 1], lse=r.lse[b:b + 1]))
+        pool = self.pool
+        rows = type("P", (), dict(Hkv=pool.Hkv, dtype=pool.dtype, k_rows=[pool.k_rows[b]], v_rows=[pool.v_rows[b]]))
+        check_prefill(rows, one, self.q[b:b + 1], [1], [self.kv[b]], Hq=self.Hq,
+                      prefix=None if prefix is None else [(pool, self.B + prefix, self.plens[prefix])])
+
+
+@pytest.mark.parametrize("n_groups", [3, 40])
+def test_prefix_groups_that_are_not_taken(cuda_lib, n_groups):
+    """A group_start that passes B, falls or is negative is flagged; the sequences of those groups have their own rows only, whatever
+    an earlier call left in the workspace, and the other groups' are right."""
+    x = Prefixed(90, [200 + 10 * (g % 3) for g in range(n_groups)], 40)
+    base = [0, 30, 60, 90] if n_groups == 3 else [2 * g for g in range(n_groups)] + [90]
+    for change in ({}, {2: 91}, {1: -1}, {0: -5}, {n_groups: 1 << 30}, {1: 70} if n_groups == 3 else {1: 5}):
+        borders = list(base)
+        for i, v in change.items():
+            borders[i] = v
+        # what a call without groups may have left there: a row whose maximum is 0 and whose sum is 1.0, 1.0, ...
+        x.records.copy_(i32([0, 0x3f800000, 0, 0] * x.B))
+        r = x.run(borders)
+        assert r.status == (1 if change else 0), (change, r.status)
+        taken = [g for g in range(n_groups) if 0 <= borders[g] <= borders[g + 1] <= x.B]
+        for b in range(x.B):
+            of = [g for g in taken if borders[g] <= b < borders[g + 1]]
+            if len(of) <= 1:              # (a start that falls puts sequences into two groups: undefined)
+                x.check(r, b, of[0] if of else None)
