@@ -47,12 +47,19 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const PagedAppendArgs
   const PagedGeom& g = a.g;
   const int t = (int)(w / warps_per_token), part = (int)(w - (long long)t * warps_per_token);
   pdl_wait();
+  if (blockIdx.x == gridDim.x - 1) {               // a block of its own: the starts of all sequences, with tokens or without
+    for (int b = threadIdx.x; b < g.B; b += blockDim.x) {
+      const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1);
+      if (s0 < 0 || s1 < s0 || s1 > g.n_tokens) paged_flag(g.status, kBadLength);
+    }
+    return;
+  }
   if (t >= g.n_tokens || t >= __ldg(a.q_start + g.B)) return;
   const int b = paged_find(a.q_start, g.B, t, lane);
   if (b < 0) { if (lane == 0) paged_flag(g.status, kBadLength); return; }
   const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1), kv = __ldg(a.kv_len + b);
   const long long at = (long long)kv - s1 + t;     // place in the cache (64 bits: the lengths may be anything)
-  if (s0 < 0 || s1 <= t || kv < 0 || at < 0 || at >= (long long)g.max_pages << g.lg_page) {
+  if (s0 < 0 || s1 <= t || s1 > g.n_tokens || kv < 0 || at < 0 || at >= (long long)g.max_pages << g.lg_page) {
     if (lane == 0) paged_flag(g.status, kBadLength);
     return;
   }
@@ -122,7 +129,7 @@ template <bool kF16, int kRows>
 cudaError_t launch(const PagedAppendArgs& a, cudaStream_t st) {
   const int n_rows = (a.q ? a.g.Hq : 0) + 2 * a.g.Hkv;
   const int warps = (n_rows + 4 * kRows - 1) / (4 * kRows);
-  const long long blocks = ((long long)a.g.n_tokens * warps + 7) / 8;
+  const long long blocks = ((long long)a.g.n_tokens * warps + 7) / 8 + 1;   // (the last looks the starts over)
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   const cudaError_t e = launch_pdl(paged_append_kernel<kF16, kRows>, dim3((unsigned)blocks), dim3(256), 0, st, a, warps);
   if (e == cudaSuccess) count_launch(1);

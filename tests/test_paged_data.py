@@ -69,3 +69,66 @@ def test_prefix_groups_that_are_not_taken(cuda_lib, n_groups):
             of = [g for g in taken if borders[g] <= b < borders[g + 1]]
             if len(of) <= 1:              # (a start that falls puts sequences into two groups: undefined)
                 x.check(r, b, of[0] if of else None)
+
+
+# ------------------------------------------------------------------------------------------ append
+class Appended:
+    """A batch in pages whose rows are all there, and new tokens for it."""
+
+    def __init__(self, kv, T, Hkv=2, page=64, spare=3):
+        self.kv, self.T, self.Hkv = kv, T, Hkv
+        self.pool = Pool(kv, Hkv=Hkv, page=page, seed=1, spare=spare)
+        self.p = cd.make_paged_params(B=len(kv), Hq=8, Hkv=Hkv, page_size=page, n_pages=self.pool.n_pages, max_pages=self.pool.max_pages)
+        g = torch.Generator().manual_seed(7)
+        self.q, self.k, self.v = (torch.randn((T, h, D), generator=g).to(BF).cuda() for h in (8, Hkv, Hkv))
+
+    def run(self, q_start, kv=None):
+        """The status, and which tokens were stored (anywhere), by their keys."""
+        K, V = self.pool.K.clone(), self.pool.V.clone()
+        ws, q_out = workspace(self.p, self.T), torch.full_like(self.q, 7.0)
+        cd.calidrop_paged_append(self.p, self.q, self.k, self.v, None, None, K, V, self.pool.table, i32(q_start), i32(kv or self.kv), q_out, ws)
+        status = status_of(ws)
+        rows = K.transpose(1, 2).reshape(-1, self.Hkv * D).view(torch.int16)
+        old = self.pool.K.transpose(1, 2).reshape(-1, self.Hkv * D).view(torch.int16)
+        changed = rows[(rows != old).any(1)]
+        keys = self.k.reshape(self.T, -1).view(torch.int16)
+        stored = (changed[:, None] == keys[None]).all(2).any(0) if len(changed) else torch.zeros(self.T, dtype=torch.bool, device="cuda")
+        assert (changed[:, None] == keys[None]).all(2).any(1).all(), "a row is no token's"
+        assert torch.equal((q_out != 7.0).flatten(1).any(1), stored)
+        return status, stored.tolist()
+
+
+@pytest.mark.parametrize("starts,taken", [
+    ([0, 10, 20, 40], range(40)),
+    ([0, 10, 20, 35], range(35)),                 # what lies behind is padding
+    ([0, 10, 20, 41], range(20)),                 # passes the tokens
+    ([0, 10, 20, 1 << 30], range(20)),
+    ([0, 30, 10, 40], None),                      # falls
+    ([0, 20, 30, 10], None),                      # falls at the end: all tokens behind it are padding
+    ([0, 20, 30, -1], ()),
+    ([-1, 10, 20, 40], None),
+    ([5, 5, 20, 40], None),
+    ([0, 1 << 30, -(1 << 30), 40], None),
+    ([41, 41, 41, 41], ()),
+    ([-3, -2, -1, 0], ()),
+])
+def test_append_starts(cuda_lib, starts, taken):
+    """The starts that calidrop_paged_prefill flags are flagged by the append, too, and the tokens of sequences that pass the end are left out."""
+    x = Appended([200, 300, 100], 40)
+    status, stored = x.run(starts)
+    good = all(0 <= a <= b <= 40 for a, b in zip(starts, starts[1:])) and starts[0] in (0, 41)
+    assert status == (0 if good else 1)
+    if taken is not None:
+        assert [t for t in range(40) if stored[t]] == list(taken)
+
+
+def test_append_starts_of_many_sequences(cuda_lib):
+    """One bad start among more sequences than a block has threads, without tokens."""
+    B = 700
+    x = Appended([5] * B, 3, spare=0)
+    base = [0] * 600 + [3] * (B + 1 - 600)
+    assert x.run(base, [5] * B)[0] == 0
+    for at, v in ((300, 4), (650, 2), (B, 4), (1, -1)):
+        starts = list(base)
+        starts[at] = v
+        assert x.run(starts)[0] == 1, (at, v)
