@@ -47,10 +47,11 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const PagedAppendArgs
   const PagedGeom& g = a.g;
   const int t = (int)(w / warps_per_token), part = (int)(w - (long long)t * warps_per_token);
   pdl_wait();
-  if (blockIdx.x == gridDim.x - 1) {               // a block of its own: the starts of all sequences, with tokens or without
+  const int cap = g.max_pages << g.lg_page;
+  if (blockIdx.x == gridDim.x - 1) {               // a block of its own: the starts and lengths of all sequences, with tokens or without
     for (int b = threadIdx.x; b < g.B; b += blockDim.x) {
-      const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1);
-      if (s0 < 0 || s1 < s0 || s1 > g.n_tokens) paged_flag(g.status, kBadLength);
+      const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1), kv = __ldg(a.kv_len + b);
+      if (s0 < 0 || s1 < s0 || s1 > g.n_tokens || kv < 0 || kv > cap) paged_flag(g.status, kBadLength);
     }
     return;
   }
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const PagedAppendArgs
   if (b < 0) { if (lane == 0) paged_flag(g.status, kBadLength); return; }
   const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1), kv = __ldg(a.kv_len + b);
   const long long at = (long long)kv - s1 + t;     // place in the cache (64 bits: the lengths may be anything)
-  if (s0 < 0 || s1 <= t || s1 > g.n_tokens || kv < 0 || at < 0 || at >= (long long)g.max_pages << g.lg_page) {
+  if (s0 < 0 || s1 <= t || s1 > g.n_tokens || kv < 0 || kv > cap || at < 0) {
     if (lane == 0) paged_flag(g.status, kBadLength);
     return;
   }

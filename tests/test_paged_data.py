@@ -132,3 +132,17 @@ def test_append_starts_of_many_sequences(cuda_lib):
         starts = list(base)
         starts[at] = v
         assert x.run(starts)[0] == 1, (at, v)
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("length", ["over", "far", "negative", "least"])
+def test_append_lengths(cuda_lib, which, length):
+    """A length beyond the table is flagged and all tokens of its sequence are left out, those whose own place lies inside it among
+    them; sequence 1 has no new tokens, and its length is looked at all the same."""
+    x = Appended([200, 300, 100], 40)
+    cap = x.pool.max_pages * 64
+    kv = [200, 300, 100]
+    kv[which] = {"over": cap + 3, "far": (1 << 31) - 1, "negative": -1, "least": -(1 << 31)}[length]
+    status, stored = x.run([0, 20, 20, 40], kv)
+    assert status == 1
+    assert stored == [which != 0] * 20 + [which != 2] * 20
