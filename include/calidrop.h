@@ -481,6 +481,10 @@ int calidrop_decode_host(const calidrop_params* p,
  *   value may also reach tokens of the same sequence that do not see it.  Elsewhere, and for K
  *   everywhere, what is masked or lies in rows and pages that are not visible has no effect,
  *   whatever it holds.
+ *
+ *   Logits, softmax sums and the sums of P V are held in 32 bits, relative to the largest logit so far: the sum of |V| over the rows
+ *   that a query sees, each with a weight of 1 at most, has to stay below 2^128 (only bf16 has such values).  P is rounded
+ *   to the type of V for the product P V, and outputs are rounded once.
  */
 #define CALIDROP_BF16 0
 #define CALIDROP_FP16 1

@@ -747,10 +747,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     }
   } else if (warp < kSoftmaxWarps) {
     // ------------------------------------------------------------ softmax: two threads to a row
-    // O is rescaled when a row's maximum has grown by more than 2^kLazy over its reference.  In bf16 as in fp32 a factor costs no
-    // bits, so that is where terms and sums are still far from the largest numbers, and hardly ever happens; in fp16 terms have to
-    // stay below 2^16 (and are kept 2^kBias higher than they are, see pack16).
-    constexpr float kBias = kF16 ? 7.f : 0.f, kLazy = kF16 ? 8.f : 40.f;
+    // O is rescaled when a row's maximum has grown by more than 2^kLazy over its reference.  In bf16 the terms are kept 2^-8 lower than
+    // they are, so that one that has grown is 1 at most and the sums of P V have the range that they have with the maximum itself
+    // (with a growth of 2^40 let pass, values of V beyond 2^87 became infinite); a factor costs no bits.  In fp16 terms have to stay
+    // below 2^16 (and are kept 2^kBias higher than they are, see pack16).
+    constexpr float kLazy = 8.f, kBias = kF16 ? 7.f : -kLazy;
     const int s = warp >> 3, half = (warp >> 2) & 1, r = tid & 127;
     const uint32_t lane_bits = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem_base + lane_bits + (uint32_t)(s * 128 + half * 64), o_addr = s_addr + kColO;

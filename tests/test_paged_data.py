@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2507_19906_b200 import binding as cd
-from paged_util import D, Pool, check_prefill, i32, queries, status_of, workspace
+from paged_util import D, Pool, check_prefill, i32, queries, run_prefill, status_of, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -146,3 +146,53 @@ def test_append_lengths(cuda_lib, which, length):
     status, stored = x.run([0, 20, 20, 40], kv)
     assert status == 1
     assert stored == [which != 0] * 20 + [which != 2] * 20
+
+
+# ------------------------------------------------------------------------------------------ the range of V
+def spread(n, Hkv, dtype, level, jump, at):
+    """Keys along one direction and queries along it: logits of `level`, and of `jump` more (log2) from row `at` on; the direction."""
+    u = torch.zeros(D)
+    u[:16] = 1.0                                            # 16 ones: products and their sums are exact in any order
+    k = torch.zeros((Hkv, n, D))
+    k[:, at:] = u * jump / 16
+    return (k + u * level / 16).to(dtype).cuda(), u.to(dtype).cuda()
+
+
+@pytest.mark.parametrize("form", ["prefill", "chunk", "decode", "prefix", "long prefix"])
+@pytest.mark.parametrize("dtype,size", [(BF, 2.0 ** 100), (BF, 2.0 ** 115), (BF, 2.0 ** -100), (BF, 2.0 ** -125), (FP, 3e4), (FP, 2.0 ** -20)])
+@pytest.mark.parametrize("jump", [7.0, 9.0, 36.0, 41.0])
+def test_large_and_small_values(cuda_lib, form, dtype, size, jump):
+    """Values of V whose sums fit into 32 bits, where the largest logit is far behind the first tile and above its maximum by just less
+    or more than a reference is left to lag."""
+    # (a long prefix of many heads is cut into chunks of several tiles: row 6100 lies inside one)
+    n, Hq, Hkv, at = (12000, 8, 8, 6100) if form == "long prefix" else (700, 8, 2, 500)
+    pool = Pool([n, 1], Hkv=Hkv, page=64, dtype=dtype, seed=6)
+    k, u = spread(n, Hkv, dtype, 1.0, jump, at)
+    pool.k_rows[0] = k
+    pool.v_rows[0] = (torch.sign(pool.v_rows[0].float()) * size * torch.linspace(0.5, 1.0, D, device="cuda")).to(dtype)
+    pool.k_rows[1], pool.v_rows[1] = k[:, :1], pool.v_rows[0][:, :1]
+    for b in range(2):
+        pool.write(b, 0, pool.k_rows[b], pool.v_rows[b])
+    scale = math.log(2.0)                                   # logits in units of log2
+    r = type("R", (), {})()
+    if form in ("prefill", "chunk"):
+        m = n if form == "prefill" else 3
+        q = u.expand(m, Hq, D).contiguous()
+        r = run_prefill(pool, q, [m], [n], Hq=Hq, scale=scale)
+        check_prefill(pool, r, q, [m], [n], Hq=Hq, scale=scale)
+        return
+    q = u.expand(1, Hq, D).contiguous()
+    p = cd.make_paged_params(B=1, Hq=Hq, Hkv=Hkv, page_size=64, n_pages=pool.n_pages, max_pages=pool.max_pages, dtype=dtype, softmax_scale=scale,
+                             n_groups=1, max_prefix_pages=pool.max_pages)
+    ws = workspace(p, 1)
+    r.out, r.lse = torch.full_like(q, 7.0), torch.full((1, Hq), 7.0, device="cuda")
+    if form == "decode":
+        cd.calidrop_paged_decode(p, q, pool.K, pool.V, pool.table, i32([n]), r.out, r.lse, ws)
+    else:
+        cd.calidrop_paged_prefix_decode(p, q, pool.K, pool.V, i32([0, 1]), pool.table, i32([n]), pool.table[1:], i32([1]), r.out, r.lse, ws)
+    assert status_of(ws) == 0
+    if form == "decode":
+        check_prefill(pool, r, q, [1], [n], Hq=Hq, scale=scale)
+    else:
+        own = type("P", (), dict(Hkv=Hkv, dtype=dtype, k_rows=pool.k_rows[1:], v_rows=pool.v_rows[1:]))
+        check_prefill(own, r, q, [1], [1], Hq=Hq, scale=scale, prefix=[(pool, 0, n)])
