@@ -9,8 +9,8 @@ constexpr int kMaxSequences = 4096;
 constexpr int kPagedTileKeys = 128;   // keys of a tile of the tensor-core attention
 constexpr int kPagedRows = 256;       // query rows of an item of it: two streams of 128
 
-// bits of the workspace's error word (waits that ran out add their own code above them)
-constexpr unsigned kBadLength = 1u, kBadPage = 2u, kBadPosition = 4u;
+// bits of the workspace's error word.  kWaitRanOut: beside the code of the wait, which is stored only where the word was 0
+constexpr unsigned kBadLength = 1u, kBadPage = 2u, kBadPosition = 4u, kWaitRanOut = 0x1000u;
 
 struct PagedGeom {
   int B, Hq, Hkv, G, n_tokens;

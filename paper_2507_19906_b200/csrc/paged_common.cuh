@@ -56,6 +56,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// Whether a wait of this CTA has run out (one thread says so in the workspace): by a bit of its own, since the word may hold those of
+// bad data already.
+__device__ __forceinline__ bool paged_aborted(const tc::Ctl& ctl) {
+  if (!ctl.abort) return false;
+  if (threadIdx.x == 0) atomicOr(ctl.status, kWaitRanOut);
+  return true;
+}
+
 // 16 consecutive fp32 columns of this thread's lane of tensor memory (see tc::tmem_ld32).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(

@@ -1020,7 +1020,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (ctl.abort) {      // a wait has run out: copies and MMAs may still be under way, and need this CTA's memory for a few microseconds
+  if (paged_aborted(ctl)) {      // copies and MMAs may still be under way, and need this CTA's memory for a few microseconds
     const long long t0 = clock64();
     while (clock64() - t0 < 400000) {}
   }

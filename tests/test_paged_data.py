@@ -196,3 +196,55 @@ def test_large_and_small_values(cuda_lib, form, dtype, size, jump):
     else:
         own = type("P", (), dict(Hkv=Hkv, dtype=dtype, k_rows=pool.k_rows[1:], v_rows=pool.v_rows[1:]))
         check_prefill(own, r, q, [1], [1], Hq=Hq, scale=scale, prefix=[(pool, 0, n)])
+
+
+# ------------------------------------------------------------------------------------------ a wait that runs out
+WAIT = r'''
+#include "paged_common.cuh"
+using namespace calidrop;
+
+// One CTA waits for a barrier at which nobody arrives, up to the limit of all waits, in a workspace whose word is `word`.
+__global__ void wait_kernel(unsigned* word, int arrive) {
+  __shared__ unsigned long long bar;
+  __shared__ tc::Ctl ctl;
+  if (threadIdx.x == 0) {
+    ctl.abort = 0;
+    ctl.status = word;
+    tc::mbar_init(smem_u32(&bar), 1);
+    tc::fence_mbar_init();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && arrive) tc::mbar_arrive(smem_u32(&bar));
+  tc::mbar_wait(&ctl, smem_u32(&bar), 0, 0x100u);
+  __syncthreads();
+  paged_aborted(ctl);
+}
+
+extern "C" int run_wait(unsigned* word, int arrive) {
+  wait_kernel<<<1, 32>>>(word, arrive);
+  return (int)cudaDeviceSynchronize();
+}
+'''
+
+
+def test_a_wait_that_runs_out_shows_beside_the_bits_of_bad_data(cuda_lib, tmp_path):
+    """The waits of the prefill kernel, and how it reports them: a barrier that nobody arrives at, two seconds."""
+    import ctypes
+    import os
+    import subprocess
+
+    from paper_2507_19906_b200 import build
+
+    src, lib = tmp_path / "wait.cu", tmp_path / "wait.so"
+    src.write_text(WAIT)
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")] + build.NVCC_FLAGS + ["-I", build.CSRC, "-o", str(lib), str(src)])
+    run = ctypes.CDLL(str(lib)).run_wait
+    for word, arrive in ((0, 1), (2, 1), (0, 0), (3, 0)):
+        w = i32([word])
+        torch.cuda.synchronize()
+        assert run(ctypes.c_void_p(w.data_ptr()), arrive) == 0
+        got = w.item()
+        if arrive:
+            assert got == word
+        else:
+            assert got & 7 == word and got & ~7, hex(got)
