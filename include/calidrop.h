@@ -476,6 +476,8 @@ int calidrop_decode_host(const calidrop_params* p,
  *   angles) is caught by the kernels: nothing is read or written out of bounds, the sequence's results
  *   are undefined and the workspace's first 32-bit word becomes non-zero (bit 0: lengths, bit 1: page,
  *   bit 2: position; other bits: a wait inside a kernel ran out).  The word stays until the caller clears it.
+ *   A wait runs out (after a second or two) only through a bug or a failing device: that call's outputs are undefined, and the whole
+ *   workspace has to be zeroed again before its next use, since the counters of work may not be back at zero.
  *
  *   Values in rows [0, kv_len) are expected to be finite in calidrop_paged_prefill: an infinite or NaN
  *   value may also reach tokens of the same sequence that do not see it.  Elsewhere, and for K
@@ -512,8 +514,9 @@ typedef struct calidrop_paged_params {
 /*
  * Bytes of scratch that every calidrop_paged_* call needs for these parameters and up to n_tokens new
  * tokens (0 if they are invalid).  256-byte aligned; zeroed once before its first use
- * (calidrop_decode_workspace_init); every call leaves it ready for the next.  Calls that overlap on
- * the device must not share a workspace; calls of different kinds may use the same one in turn.
+ * (calidrop_decode_workspace_init); every call leaves it ready for the next, unless a wait ran out (see
+ * above).  Calls that overlap on the device must not share a workspace; calls of different kinds may use
+ * the same one in turn.
  */
 size_t calidrop_paged_workspace_bytes(const calidrop_paged_params* p, int32_t n_tokens);
 
