@@ -169,13 +169,25 @@ struct Args {
     }
     return ptr(i);
   }
+  // The tensor that an argument is, of a subclass or not; null: it is none, or None, or an address.
+  const at::Tensor* tensor(int i) {
+    PyObject* o = a[i];
+    if (!ok || o == Py_None || PyLong_Check(o)) return nullptr;
+    if (!THPVariable_CheckExact(o)) {
+      const int is = THPVariableClass ? PyObject_IsInstance(o, THPVariableClass) : 0;
+      if (is < 0) ok = false;
+      if (is <= 0) return nullptr;
+    }
+    return &THPVariable_Unpack(o);
+  }
   // No tensor of another device, and none of the host's: its address would mean nothing to the kernels.
   void on_this_device(Py_ssize_t n) {
     int device = -1;                     // the current one, asked for once
     for (Py_ssize_t i = 1; ok && i < n; ++i) {
-      if (!THPVariable_CheckExact(a[i])) continue;
+      const at::Tensor* const x = tensor(i);
+      if (!x) continue;
       try {
-        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        const at::Tensor& t = *x;
         if (t.is_cuda() && device < 0) device = c10::cuda::current_device();
         if (t.is_cuda() && t.get_device() == device) continue;
         PyErr_SetString(PyExc_ValueError, "tensors on the current CUDA device expected");
