@@ -23,6 +23,7 @@ namespace {
 #define DECLARE(name) decltype(&calidrop_##name) f_##name = nullptr;
 CALIDROP_ENTRIES(DECLARE)
 #undef DECLARE
+decltype(&calidrop_paged_workspace_bytes) f_paged_workspace_bytes = nullptr;
 
 PyTypeObject* params_type = nullptr;   // the binding's ctypes structures (see open)
 PyTypeObject* layer_type = nullptr;
@@ -197,6 +198,13 @@ struct Args {
       ok = false;
     }
   }
+  // Tensors hold elements of the type that the library reads there (what an address points at is the caller's word).
+  void type(int i, const char* name, at::ScalarType want) {
+    const at::Tensor* const x = tensor(i);
+    if (!x || x->scalar_type() == want) return;
+    PyErr_Format(PyExc_ValueError, "%s has elements of type %s, %s expected", name, c10::toString(x->scalar_type()), c10::toString(want));
+    ok = false;
+  }
   // the first dimension of a tensor
   int32_t tokens(int i) {
     if (ok && THPVariable_CheckExact(a[i])) {
@@ -280,10 +288,47 @@ ENTRY(decode_batched, 4, x.params(0), (int32_t)x.len(1), x.layers(1), x.i32(2), 
 ENTRY(decode_static, 13, x.params(0), x.ptr(1), x.ptr(2), x.ptr(3), x.ptr(4), x.ptr(5), x.i32(6), (const float*)x.ptr(7),
       (const float*)x.ptr(8), x.ptr(9), x.ptr(10), (float*)x.ptr(11), (uint8_t*)x.ptr(12))
 
+// What the arguments of the entry points over a cache in pages have to be.  Parameters that the library refuses are left to it.
+struct PagedCheck {
+  Args& x;
+  const calidrop_paged_params* p;
+  const at::ScalarType half;
+  PagedCheck(Args& x, const calidrop_paged_params* p)
+      : x(x), p(p), half(p && p->dtype == CALIDROP_FP16 ? at::kHalf : at::kBFloat16) {}
+  void heads(int i, const char* name) { x.type(i, name, half); }                     // queries, keys, values, pages and outputs
+  void ints(int i, const char* name) { x.type(i, name, at::kInt); }
+  void floats(int i, const char* name) { x.type(i, name, at::kFloat); }
+};
+
+void check_paged_append(PagedCheck c) {
+  c.heads(1, "q"); c.heads(2, "k"); c.heads(3, "v");
+  c.ints(4, "positions"); c.floats(5, "cos_sin");
+  c.heads(6, "K_pages"); c.heads(7, "V_pages");
+  c.ints(8, "block_table"); c.ints(9, "q_start"); c.ints(10, "kv_len");
+  c.heads(11, "q_out");
+}
+void check_paged_prefill(PagedCheck c) {
+  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
+  c.ints(4, "block_table"); c.ints(5, "q_start"); c.ints(6, "kv_len");
+  c.heads(7, "out"); c.floats(8, "lse");
+}
+void check_paged_decode(PagedCheck c) {
+  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
+  c.ints(4, "block_table"); c.ints(5, "kv_len");
+  c.heads(6, "out"); c.floats(7, "lse");
+}
+void check_paged_prefix_decode(PagedCheck c) {
+  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
+  c.ints(4, "group_start"); c.ints(5, "prefix_table"); c.ints(6, "prefix_len");
+  c.ints(7, "block_table"); c.ints(8, "kv_len");
+  c.heads(9, "out"); c.floats(10, "lse");
+}
+
 #define PAGED_ENTRY(name, n_args, ...)                                                  \
   PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {                 \
     Args x(args, n, n_args);                                                            \
     const calidrop_paged_params* p = x.paged(0);                                        \
+    if (x.ok && f_paged_workspace_bytes(p, 0)) check_##name(PagedCheck(x, p));          \
     x.on_this_device(n);                                                                \
     if (!x.ok) return nullptr;                                                          \
     return forward(x, f_##name, p, __VA_ARGS__);                                        \
@@ -325,6 +370,7 @@ PyObject* py_open(PyObject*, PyObject* const* args, Py_ssize_t n) {
   f_##name = (decltype(f_##name))dlsym(h, "calidrop_" #name);                                        \
   if (!f_##name) return PyErr_Format(PyExc_ImportError, "%s does not export calidrop_" #name, s);
   CALIDROP_ENTRIES(RESOLVE)
+  RESOLVE(paged_workspace_bytes)
 #undef RESOLVE
   params_type = (PyTypeObject*)Py_NewRef(args[1]);
   layer_type = (PyTypeObject*)Py_NewRef(args[2]);
