@@ -205,6 +205,24 @@ struct Args {
     PyErr_Format(PyExc_ValueError, "%s has elements of type %s, %s expected", name, c10::toString(x->scalar_type()), c10::toString(want));
     ok = false;
   }
+  // ... and n rows of `row` elements.  A tensor whose dimensions behind the first make a row, `stride` elements apart (0: packed), has as
+  // many as its first dimension says; of one in another shape that is packed the elements are counted (`shaped`: only of a single
+  // row or a flat tensor, since the rows of a table would lie elsewhere).
+  void size(int i, const char* name, int64_t n, int64_t row, int64_t stride = 0, bool shaped = false) {
+    const at::Tensor* const x = tensor(i);
+    if (!x) return;
+    const int64_t dims = x->dim(), all = x->numel(), first = dims > 0 ? x->size(0) : 1;
+    bool by_rows = dims > 0;
+    if (by_rows) {
+      int64_t behind = 1;
+      for (int64_t d = 1; d < dims; ++d) behind *= x->size(d);
+      by_rows = behind == row;
+    }
+    const bool counted = (stride == 0 || stride == row) && (!shaped || n <= 1 || dims <= 1);
+    if (by_rows ? first >= n : counted && all >= n * row) return;
+    PyErr_Format(PyExc_ValueError, "%s is too small or of another shape: %lld rows of %lld elements expected", name, (long long)n, (long long)row);
+    ok = false;
+  }
   // the first dimension of a tensor
   int32_t tokens(int i) {
     if (ok && THPVariable_CheckExact(a[i])) {
@@ -288,60 +306,90 @@ ENTRY(decode_batched, 4, x.params(0), (int32_t)x.len(1), x.layers(1), x.i32(2), 
 ENTRY(decode_static, 13, x.params(0), x.ptr(1), x.ptr(2), x.ptr(3), x.ptr(4), x.ptr(5), x.i32(6), (const float*)x.ptr(7),
       (const float*)x.ptr(8), x.ptr(9), x.ptr(10), (float*)x.ptr(11), (uint8_t*)x.ptr(12))
 
-// What the arguments of the entry points over a cache in pages have to be.  Parameters that the library refuses are left to it.
+// What the tensors of the entry points over a cache in pages have to be.  Parameters that the library refuses are left to it.
 struct PagedCheck {
   Args& x;
   const calidrop_paged_params* p;
+  int64_t n;                                           // tokens
   const at::ScalarType half;
-  PagedCheck(Args& x, const calidrop_paged_params* p)
-      : x(x), p(p), half(p && p->dtype == CALIDROP_FP16 ? at::kHalf : at::kBFloat16) {}
-  void heads(int i, const char* name) { x.type(i, name, half); }                     // queries, keys, values, pages and outputs
-  void ints(int i, const char* name) { x.type(i, name, at::kInt); }
-  void floats(int i, const char* name) { x.type(i, name, at::kFloat); }
+  PagedCheck(Args& x, const calidrop_paged_params* p, int64_t n)
+      : x(x), p(p), n(n), half(p->dtype == CALIDROP_FP16 ? at::kHalf : at::kBFloat16) {}
+  void heads(int i, const char* name, int64_t count, int64_t stride = 0) {             // of the tokens
+    x.type(i, name, half);
+    x.size(i, name, n, count * p->D, stride);
+  }
+  void pages(int i, const char* name) {
+    x.type(i, name, half);
+    const at::Tensor* const t = x.tensor(i);
+    if (t && t->dim() == 4 && (t->size(1) != p->Hkv || t->size(2) != p->page_size || t->size(3) != p->D)) {
+      PyErr_Format(PyExc_ValueError, "%s: pages of [Hkv][page_size][D] elements expected", name);
+      x.ok = false;
+    }
+    x.size(i, name, p->n_pages, (int64_t)p->Hkv * p->page_size * p->D, p->page_stride);
+  }
+  void ints(int i, const char* name, int64_t count) {
+    x.type(i, name, at::kInt);
+    x.size(i, name, count, 1);
+  }
+  void table(int i, const char* name, int64_t count, int64_t row) {
+    x.type(i, name, at::kInt);
+    x.size(i, name, count, row, 0, true);
+  }
+  void floats(int i, const char* name, int64_t count, int64_t row, bool shaped) {
+    x.type(i, name, at::kFloat);
+    x.size(i, name, count, row, 0, shaped);
+  }
 };
 
 void check_paged_append(PagedCheck c) {
-  c.heads(1, "q"); c.heads(2, "k"); c.heads(3, "v");
-  c.ints(4, "positions"); c.floats(5, "cos_sin");
-  c.heads(6, "K_pages"); c.heads(7, "V_pages");
-  c.ints(8, "block_table"); c.ints(9, "q_start"); c.ints(10, "kv_len");
-  c.heads(11, "q_out");
+  const calidrop_paged_params* p = c.p;
+  c.heads(1, "q", p->Hq, p->q_stride); c.heads(2, "k", p->Hkv, p->k_stride); c.heads(3, "v", p->Hkv, p->v_stride);
+  c.ints(4, "positions", c.n);
+  if (p->rot_dim) c.floats(5, "cos_sin", p->max_pos, p->rot_dim, true);
+  c.pages(6, "K_pages"); c.pages(7, "V_pages");
+  c.table(8, "block_table", p->B, p->max_pages); c.ints(9, "q_start", (int64_t)p->B + 1); c.ints(10, "kv_len", p->B);
+  if (c.x.a[1] != Py_None) c.heads(11, "q_out", p->Hq);
 }
 void check_paged_prefill(PagedCheck c) {
-  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
-  c.ints(4, "block_table"); c.ints(5, "q_start"); c.ints(6, "kv_len");
-  c.heads(7, "out"); c.floats(8, "lse");
+  const calidrop_paged_params* p = c.p;
+  c.heads(1, "q", p->Hq, p->q_stride); c.pages(2, "K_pages"); c.pages(3, "V_pages");
+  c.table(4, "block_table", p->B, p->max_pages); c.ints(5, "q_start", (int64_t)p->B + 1); c.ints(6, "kv_len", p->B);
+  c.heads(7, "out", p->Hq); c.floats(8, "lse", c.n, p->Hq, false);
 }
 void check_paged_decode(PagedCheck c) {
-  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
-  c.ints(4, "block_table"); c.ints(5, "kv_len");
-  c.heads(6, "out"); c.floats(7, "lse");
+  const calidrop_paged_params* p = c.p;
+  c.heads(1, "q", p->Hq, p->q_stride); c.pages(2, "K_pages"); c.pages(3, "V_pages");
+  c.table(4, "block_table", p->B, p->max_pages); c.ints(5, "kv_len", p->B);
+  c.heads(6, "out", p->Hq); c.floats(7, "lse", c.n, p->Hq, false);
 }
 void check_paged_prefix_decode(PagedCheck c) {
-  c.heads(1, "q"); c.heads(2, "K_pages"); c.heads(3, "V_pages");
-  c.ints(4, "group_start"); c.ints(5, "prefix_table"); c.ints(6, "prefix_len");
-  c.ints(7, "block_table"); c.ints(8, "kv_len");
-  c.heads(9, "out"); c.floats(10, "lse");
+  const calidrop_paged_params* p = c.p;
+  c.heads(1, "q", p->Hq, p->q_stride); c.pages(2, "K_pages"); c.pages(3, "V_pages");
+  c.ints(4, "group_start", (int64_t)p->n_groups + 1); c.table(5, "prefix_table", p->n_groups, p->max_prefix_pages);
+  c.ints(6, "prefix_len", p->n_groups);
+  c.table(7, "block_table", p->B, p->max_pages); c.ints(8, "kv_len", p->B);
+  c.heads(9, "out", p->Hq); c.floats(10, "lse", c.n, p->Hq, false);
 }
 
-#define PAGED_ENTRY(name, n_args, ...)                                                  \
+#define PAGED_ENTRY(name, n_args, n_tokens, ...)                                                  \
   PyObject* py_##name(PyObject*, PyObject* const* args, Py_ssize_t n) {                 \
     Args x(args, n, n_args);                                                            \
     const calidrop_paged_params* p = x.paged(0);                                        \
-    if (x.ok && f_paged_workspace_bytes(p, 0)) check_##name(PagedCheck(x, p));          \
+    const int32_t count = x.ok ? n_tokens : 0;                                          \
+    if (x.ok && f_paged_workspace_bytes(p, 0)) check_##name(PagedCheck(x, p, count));   \
     x.on_this_device(n);                                                                \
     if (!x.ok) return nullptr;                                                          \
     return forward(x, f_##name, p, __VA_ARGS__);                                        \
   }
-PAGED_ENTRY(paged_append, 13, x.tokens(2), x.rows(1, p->q_stride), x.rows(2, p->k_stride), x.rows(3, p->v_stride),
+PAGED_ENTRY(paged_append, 13, x.tokens(2), count, x.rows(1, p->q_stride), x.rows(2, p->k_stride), x.rows(3, p->v_stride),
             (const int32_t*)x.ptr(4), (const float*)x.ptr(5), x.rows(6, p->page_stride), x.rows(7, p->page_stride),
             (const int32_t*)x.ptr(8), (const int32_t*)x.ptr(9), (const int32_t*)x.ptr(10), x.ptr(11), x.ptr(12), x.nbytes(12))
-PAGED_ENTRY(paged_prefill, 10, x.tokens(1), x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+PAGED_ENTRY(paged_prefill, 10, x.tokens(1), count, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
             (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), (const int32_t*)x.ptr(6), x.ptr(7), (float*)x.ptr(8), x.ptr(9),
             x.nbytes(9))
-PAGED_ENTRY(paged_decode, 9, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+PAGED_ENTRY(paged_decode, 9, p->B, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
             (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), x.ptr(6), (float*)x.ptr(7), x.ptr(8), x.nbytes(8))
-PAGED_ENTRY(paged_prefix_decode, 12, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
+PAGED_ENTRY(paged_prefix_decode, 12, p->B, x.rows(1, p->q_stride), x.rows(2, p->page_stride), x.rows(3, p->page_stride),
             (const int32_t*)x.ptr(4), (const int32_t*)x.ptr(5), (const int32_t*)x.ptr(6), (const int32_t*)x.ptr(7),
             (const int32_t*)x.ptr(8), x.ptr(9), (float*)x.ptr(10), x.ptr(11), x.nbytes(11))
 

@@ -85,3 +85,61 @@ def test_element_types(entry, name):
         x = torch.zeros(shape, dtype=BF)
         with pytest.raises(ValueError, match=f"{name} has elements of type BFloat16, Half expected"):
             call(entry, arguments(entry, torch.float16, **{name: x}), dtype=torch.float16)
+
+
+def shorter(t, s, dim):
+    return torch.zeros(tuple(n - (d == dim) for d, n in enumerate(s)), dtype=BF if t == "half" else t)
+
+
+# (the tokens of append and prefill are counted by k and q)
+@pytest.mark.parametrize("entry,name", [c for c in CASES if c not in (("append", "k"), ("prefill", "q"))])
+def test_too_few_rows(entry, name):
+    kind, shape = next((t, s) for n, t, s in ENTRIES[entry] if n == name)
+    with pytest.raises(ValueError, match=f"{name} is too small"):
+        call(entry, arguments(entry, **{name: shorter(kind, shape, 0)}))
+    with pytest.raises(ValueError, match=f"{name} is too small"):
+        call(entry, arguments(entry, **{name: shorter(kind, shape, 0).flatten()}))
+    # more rows are no fault, and where all is packed their dimensions neither
+    more = torch.zeros((shape[0] + 3, *shape[1:]), dtype=BF if kind == "half" else kind)
+    for x in (more, more.flatten()):
+        with pytest.raises(ValueError, match="CUDA device"):
+            call(entry, arguments(entry, **{name: x}))
+
+
+@pytest.mark.parametrize("entry,name", [c for c in CASES if c[1] not in ("positions", "q_start", "kv_len", "group_start", "prefix_len")])
+def test_rows_of_another_length(entry, name):
+    kind, shape = next((t, s) for n, t, s in ENTRIES[entry] if n == name)
+    with pytest.raises(ValueError, match=f"^{name}"):
+        call(entry, arguments(entry, **{name: shorter(kind, shape, 1)}))
+
+
+@pytest.mark.parametrize("entry", ENTRIES)
+def test_tables_and_pages_in_another_layout(entry):
+    wide = torch.zeros((B, MAX_PAGES + 1), dtype=I32)
+    with pytest.raises(ValueError, match="^block_table"):
+        call(entry, arguments(entry, block_table=wide))
+    swapped = torch.zeros((N_PAGES, PAGE, HKV, D), dtype=BF)
+    for name in ("K_pages", "V_pages"):
+        with pytest.raises(ValueError, match=f"^{name}"):
+            call(entry, arguments(entry, **{name: swapped}))
+    # of a single sequence's table the rest is not looked at
+    one = dict(block_table=torch.zeros((1, MAX_PAGES + 1), dtype=I32), group_start=torch.zeros(2, dtype=I32))
+    with pytest.raises(ValueError, match="CUDA device"):
+        call(entry, arguments(entry, **{k: v for k, v in one.items() if k in [n for n, *_ in ENTRIES[entry]]}), B=1)
+
+
+def test_strided_queries_and_halves_of_a_pool():
+    """The views that the parameters' strides describe, and those that they do not."""
+    x = torch.zeros((T, HQ + 2 * HKV, D), dtype=BF)
+    q, k, v = x[:, :HQ], x[:, HQ:HQ + HKV], x[:, HQ + HKV:]
+    both = torch.zeros((N_PAGES, 2, HKV, PAGE, D), dtype=BF)
+    strides = dict(q_stride=q.stride(0), k_stride=k.stride(0), v_stride=v.stride(0), page_stride=both.stride(0))
+    args = arguments("append", q=q, k=k, v=v, K_pages=both[:, 0], V_pages=both[:, 1])
+    with pytest.raises(ValueError, match="CUDA device"):
+        call("append", args, **strides)
+    with pytest.raises(ValueError, match="^q is too small"):          # fewer tokens than keys
+        call("append", [q[:-1]] + args[1:], **strides)
+    with pytest.raises(ValueError, match="^q is too small"):          # a flat tensor has no stride between its tokens
+        call("append", [torch.zeros(x.numel(), dtype=BF)] + args[1:], **strides)
+    with pytest.raises(ValueError, match="CUDA device"):              # no queries: what stands for their output is not looked at
+        call("append", [None] + args[1:9] + [args[9], torch.zeros(1, dtype=BF), args[11]], **strides)
