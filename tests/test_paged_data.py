@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2507_19906_b200 import binding as cd
-from paged_util import D, Pool, check_prefill, i32, queries, run_prefill, status_of, workspace
+from paged_util import D, Pool, attention64, check_prefill, check_rows, i32, queries, run_prefill, status_of, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -248,3 +248,77 @@ def test_a_wait_that_runs_out_shows_beside_the_bits_of_bad_data(cuda_lib, tmp_pa
             assert got == word
         else:
             assert got & 7 == word and got & ~7, hex(got)
+
+
+# ------------------------------------------------------------------------------------------ more of the shared prefix
+@pytest.mark.parametrize("what,bit", [("prefix page", 2), ("low prefix page", 2), ("page", 2), ("prefix length", 1), ("negative prefix length", 1),
+                                      ("length", 1), ("negative length", 1)])
+@pytest.mark.parametrize("members", [1, 20])
+def test_bad_data_of_a_prefix_decode(cuda_lib, what, bit, members):
+    """Flagged, and right for the sequences that it does not concern: the second group's, and in the first those whose own rows are not bad."""
+    B = 2 * members
+    x = Prefixed(B, [300, 260], 70)
+    plens, kv = list(x.plens), list(x.kv)
+    own = "prefix" not in what
+    if what == "prefix page":
+        x.prefix_table[0, 3] = x.pool.n_pages
+    elif what == "low prefix page":
+        x.prefix_table[0, 3] = -1
+    elif what == "page":
+        x.table[0, 0] = x.pool.n_pages + 5
+    elif what.endswith("prefix length"):
+        plens[0] = -3 if what.startswith("negative") else x.pool.max_pages * 32 + 1
+        x.prefix_table[0].clamp_(min=0)             # a length is held to the table, and pages of it that exist are read
+    else:
+        kv[0] = -3 if what.startswith("negative") else x.pool.max_pages * 32 + 1
+        x.table[0].clamp_(min=0)
+    r = x.run([0, members, B], plens, kv)
+    assert r.status == bit
+    for b in range(1 if own else members, B):
+        x.check(r, b, b // members)
+
+
+def test_prefix_decode_repeats_itself(cuda_lib):
+    """Bit for bit, in one workspace, whatever another call has left there."""
+    x = Prefixed(60, [3000, 700, 64], 90, Hq=32, Hkv=8, page=64)
+    first = x.run([0, 20, 59, 60])
+    for b in (0, 19, 20, 58, 59):
+        x.check(first, b, (b >= 20) + (b >= 59))
+    for i in range(20):
+        if i % 2:
+            x.run([0, 1, 30, 31], kv=[1] * 60)
+        r = x.run([0, 20, 59, 60])
+        assert r.status == 0 and torch.equal(r.out, first.out) and torch.equal(r.lse, first.lse), i
+
+
+@pytest.mark.parametrize("form", ["prefill", "decode", "prefix"])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_a_key_at_minus_infinity_drops_out(cuda_lib, form, dtype):
+    """Logits of -inf weigh nothing, in the first tile, inside one and at the end; a token that sees no others gets zeros."""
+    n, Hq, Hkv = 300, 8, 2
+    G = Hq // Hkv
+    pool = Pool([n, 1], Hkv=Hkv, page=64, dtype=dtype, seed=1)
+    gone = torch.zeros(n, dtype=torch.bool, device="cuda")
+    gone[[0, 1, 129, 200, n - 1]] = True
+    finite = pool.k_rows[0].clone()
+    pool.k_rows[0][:, gone, 0] = -math.inf
+    pool.write(0, 0, pool.k_rows[0], pool.v_rows[0])
+    finite[:, gone] = 0
+    T = n if form == "prefill" else 1
+    q = queries(T, Hq, dtype, 2)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    p = cd.make_paged_params(B=1, Hq=Hq, Hkv=Hkv, page_size=64, n_pages=pool.n_pages, max_pages=pool.max_pages, dtype=dtype, n_groups=1,
+                             max_prefix_pages=pool.max_pages)
+    ws, out, lse = workspace(p, T), torch.full_like(q, 7.0), torch.full((T, Hq), 7.0, device="cuda")
+    if form == "prefill":
+        cd.calidrop_paged_prefill(p, q, pool.K, pool.V, pool.table, i32([0, n]), i32([n]), out, lse, ws)
+    elif form == "decode":
+        cd.calidrop_paged_decode(p, q, pool.K, pool.V, pool.table, i32([n]), out, lse, ws)
+    else:
+        cd.calidrop_paged_prefix_decode(p, q, pool.K, pool.V, i32([0, 1]), pool.table, i32([n]), pool.table[1:], i32([0]), out, lse, ws)
+    assert status_of(ws) == 0
+    t = torch.arange(n, device="cuda")
+    seen = (t <= (t if form == "prefill" else t[-1:])[:, None]) & ~gone
+    for hq in range(Hq):
+        ref = attention64(q[:, hq], finite[hq // G], pool.v_rows[0][hq // G], seen, 1 / math.sqrt(D))
+        check_rows(out[:, hq], lse[:, hq], ref, dtype, n, f"head {hq}")
