@@ -140,8 +140,10 @@ cudaError_t launch(const PagedAppendArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st) {
-  // (rows of a lane one, two, four: 256 tokens of 48 rows 3.6, 4.6, 5.5 us; 16284 of 36 rows two 60, four 57)
-  const bool many = (long long)a.g.n_tokens * ((a.q ? a.g.Hq : 0) + 2 * a.g.Hkv) > 16 * 1024;
+  // One row a lane or four: the former while its warps are all resident at once, up to about 27 thousand rows.  Measured, us, one / four,
+  // with 48, 36 and 12 rows a token: 12 thousand rows 3.5 / 4.1, 3.5 / 3.8, 3.7 / 4.0; 24 thousand 4.1 / 4.6, 4.1 / 4.3, 4.1 / 4.3; 28 thousand
+  // 5.0 / 4.7, 4.9 / 4.4, 5.2 / 4.5; 128 thousand 15.7 / 13.2, 15.8 / 14.2, 16.4 / 14.2.  (Two rows a lane: 586 thousand rows 60, four 57.)
+  const bool many = (long long)a.g.n_tokens * ((a.q ? a.g.Hq : 0) + 2 * a.g.Hkv) > 26 * 1024;
   if (a.g.f16) return many ? launch<true, 4>(a, st) : launch<true, 1>(a, st);
   return many ? launch<false, 4>(a, st) : launch<false, 1>(a, st);
 }

@@ -5,7 +5,9 @@ import pytest
 import torch
 
 from paper_2507_19906_b200 import binding as cd
-from paged_util import D, Pool, attention64, check_prefill, check_rows, i32, queries, run_prefill, status_of, workspace
+from paged_util import (D, HALF, SMALL, Pool, attention64, check_prefill, check_rows, i32, queries, run_prefill, starts, status_of,
+                        workspace)
+from test_paged import table_of_angles, turned64
 
 pytestmark = pytest.mark.gpu
 
@@ -322,3 +324,43 @@ def test_a_key_at_minus_infinity_drops_out(cuda_lib, form, dtype):
     for hq in range(Hq):
         ref = attention64(q[:, hq], finite[hq // G], pool.v_rows[0][hq // G], seen, 1 / math.sqrt(D))
         check_rows(out[:, hq], lse[:, hq], ref, dtype, n, f"head {hq}")
+
+
+# ------------------------------------------------------------------------------------------ long appends
+@pytest.mark.parametrize("dtype,Hq,Hkv,T,rot,interleaved,page", [
+    (BF, 32, 8, 553, 128, False, 64),            # just below the number of rows from which a lane takes four
+    (BF, 32, 8, 556, 128, False, 64),            # and just above
+    (BF, 28, 4, 901, 64, True, 16),
+    (FP, 5, 1, 5001, 96, False, 128),            # seven rows a token: most lanes have fewer than four
+    (FP, 16, 16, 700, 128, True, 256),
+])
+@pytest.mark.parametrize("with_q", [True, False])
+def test_long_appends(cuda_lib, dtype, Hq, Hkv, T, rot, interleaved, page, with_q):
+    """Both forms of the kernel, against the definition."""
+    if not with_q:
+        T = T * (Hq + 2 * Hkv) // (2 * Hkv)                  # as many rows
+    lens = [T // 3, 0, T - T // 3 - 1, 1]
+    old = [7, 30, 0, 70]
+    kv = [a + b for a, b in zip(lens, old)]
+    pool = Pool(kv, Hkv=Hkv, page=page, dtype=dtype, seed=2)
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn((T, h, D), generator=g).to(dtype).cuda() for h in (Hq, Hkv, Hkv))
+    cs = table_of_angles(max(kv), rot)
+    p = cd.make_paged_params(B=4, Hq=Hq, Hkv=Hkv, page_size=page, n_pages=pool.n_pages, max_pages=pool.max_pages, dtype=dtype, rot_dim=rot,
+                             interleaved=interleaved, max_pos=max(kv))
+    ws, q_out = workspace(p, T), torch.full((T, Hq, D), 7.0, dtype=dtype, device="cuda")
+    cd.calidrop_paged_append(p, q if with_q else None, k, v, None, cs, pool.K, pool.V, pool.table, starts(lens), i32(kv), q_out, ws)
+    assert status_of(ws) == 0
+    place = torch.cat([torch.arange(o, o + n) for o, n in zip(old, lens)]).cuda()
+    got_k, got_v = (torch.cat([pool.read(x, b, kv[b])[:, old[b]:].transpose(0, 1) for b in range(4)]) for x in (pool.K, pool.V))
+    assert torch.equal(got_v, v)
+    for got, x in [(got_k, k)] + ([(q_out, q)] if with_q else []):
+        ref, size = turned64(x, cs[place], rot, interleaved)
+        # two products and a sum in 32 bits (each half a step of 2^-23), then the rounding
+        assert ((got.double() - ref).abs() <= HALF[dtype] * ref.abs() + 3 * 2.0 ** -24 * size + SMALL[dtype]).all()
+        assert torch.equal(got[..., rot:], x[..., rot:])
+    for b in range(4):                                        # the rows ahead are as they were
+        assert torch.equal(pool.read(pool.K, b, old[b]), pool.k_rows[b][:, :old[b]])
+        assert torch.equal(pool.read(pool.V, b, old[b]), pool.v_rows[b][:, :old[b]])
+    if not with_q:
+        assert (q_out == 7.0).all()
