@@ -551,7 +551,8 @@ int calidrop_paged_append(const calidrop_paged_params* p, int32_t n_tokens, cons
  *   out      out [n_tokens][Hq][D], packed
  *   lse      out [n_tokens][Hq] f32 or NULL: natural logarithm of the softmax denominator
  * A token that sees no key (its position is negative: kv_len[b] is less than the number of new tokens)
- * gets out = 0, lse = -inf.  The last window rows of `lse`, transposed, are the lse_obs of calidrop_compress.
+ * gets out = 0, lse = -inf.  The last window rows of `lse`, transposed, are the lse_obs of calidrop_compress
+ * (which takes contiguous keys and values: those of a prompt in pages have to be gathered for it).
  * Errors as above.
  */
 int calidrop_paged_prefill(const calidrop_paged_params* p, int32_t n_tokens, const void* q, const void* K_pages,

@@ -336,6 +336,8 @@ def calidrop_decode_static(p, q, k_new, v_new, K_kept, V_kept, kv_len, O_c, LSE_
     return rc
 
 
+# The entry points over a cache in pages hold their tensors to the parameters' element types, sizes and layouts, and to the current
+# device (ValueError; AssertionError for strides).  An address in a tensor's place is taken as it is.
 PAGED_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 

@@ -7,8 +7,8 @@
 // the partners of a rotation by halves (elements 8j.. and rot/2 + 8j..), so no value crosses lanes.  The angles of a lane are
 // the same for all heads and stay in registers.  Few tokens (a decode step) take a warp per four rows, so that nothing waits for
 // a second row; many take four rows a lane, whose loads are in flight together: 16284 tokens of 36 heads out of a fused projection, 308 MB, 57 us
-// (82 % of the copy bandwidth; written rows of 256 bytes are scattered over the heads' pages).  A step of 8 tokens takes 3.3 us, the
-// pace at which the host calls, one of 256 tokens 3.7.  Rows asked for ahead of the look-up: no gain.
+// (82 % of the copy bandwidth; written rows of 256 bytes are scattered over the heads' pages).  A step of 8 tokens takes 3.2 to 3.8 us, the
+// pace at which the host calls, one of 256 tokens 3.7 to 4.2.  Rows asked for ahead of the look-up: no gain.
 #include "paged_common.cuh"
 
 namespace calidrop {

@@ -35,7 +35,7 @@ constexpr int kStride = kPagedPartStride;              // floats of a warp's par
 // What a unit costs beside its rows, in blocks.  With 1, 2, 3: 768 short units and their prefix 78, 73, 73 us, 64 of them 27.5, 26.0, 27.7, 256 long units
 // 140, 141, 140.
 constexpr int kUnitCost = 2;
-constexpr int kMinShare = 2;                           // of a CTA's part of the line: at least one block of a unit
+constexpr int kMinShare = 2;                           // of a CTA's part of the line, which may hold nothing but the places of a unit that have no rows
 // What is in shared memory behind the ring.
 struct Tail {
   float part[kStreamWarps][kMaxG][kStride];            // of the warps, at the end of a unit

@@ -20,9 +20,10 @@
 // P is handed over in two parts, of 48 keys and 16, so that little of P V is left when the last is done.
 //
 // What bounds it: for long prompts the power limit, behind it the chain of a stream's step (S, its way to the registers, the exponentials, P,
-// P V: 3000 cycles for two streams where the tensor cores need 2048); causal, 32 heads x 8192 tokens take 501 to 511 us from box to box
-// (1.08 PFLOP/s; 567 with a thread to a row, which held 128 logits and worked on few exponentials at a time).  For short prompts the chain of
-// a launch: 6 us of start, list and first loads, and 3 at the end.  For a prefix shared by few rows the memory (64 KB a step and SM in 1.4 us).
+// P V: 3000 cycles for two streams where the tensor cores need 2048); causal, 32 heads x 8192 tokens take 501 to 516 us from box to box
+// (1.08 PFLOP/s; 567 with a thread to a row, which held 128 logits and worked on few exponentials at a time).  For short prompts the longest
+// tile (1024 tokens: eight steps where the mean of an SM is four) and the launch: 6 us of start, list and first loads, and 3 at the end.  For a prefix
+// shared by few rows the memory (64 KB a step and SM in 1.4 us) and shares that are rounded down (pieces of 15 steps for a mean of 10).
 #include <algorithm>
 
 #include "exp2.cuh"

@@ -73,6 +73,25 @@ def test_prefix_groups_that_are_not_taken(cuda_lib, n_groups):
                 x.check(r, b, of[0] if of else None)
 
 
+@pytest.mark.parametrize("n_groups", [5, 41])
+def test_prefix_groups_that_lie_over_one_another(cuda_lib, n_groups):
+    """Starts that fall all the time, between groups that are each good: flagged.  With more groups than a warp counts, their tiles are
+    more than starts that do not fall could have: the list of work is given up, and all sequences have their own rows only."""
+    x = Prefixed(96, [200] * n_groups, 40, Hq=16, Hkv=2)
+    borders = [0, 96] * (n_groups // 2 + 1)
+    for _ in range(3):
+        x.records.copy_(i32([0, 0x3f800000, 0, 0] * x.B))
+        r = x.run(borders[:n_groups + 1])
+        assert r.status == 1
+        if n_groups > 32:
+            for b in (0, 1, 50, 95):
+                x.check(r, b, None)
+    r = x.run([0] * n_groups + [96])               # and the same workspace is ready for starts that do not fall
+    assert r.status == 0
+    for b in (0, 1, 50, 95):
+        x.check(r, b, n_groups - 1)
+
+
 # ------------------------------------------------------------------------------------------ append
 class Appended:
     """A batch in pages whose rows are all there, and new tokens for it."""
