@@ -43,12 +43,13 @@ template <bool kF16, int kRows>
 __global__ void __launch_bounds__(256) paged_append_kernel(const PagedAppendArgs a, int warps_per_token) {
   pdl_trigger();
   const int lane = threadIdx.x & 31;
-  const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const long long w = ((long long)(blockIdx.x - 1) * blockDim.x + threadIdx.x) >> 5;
   const PagedGeom& g = a.g;
   const int t = (int)(w / warps_per_token), part = (int)(w - (long long)t * warps_per_token);
   pdl_wait();
   const int cap = g.max_pages << g.lg_page;
-  if (blockIdx.x == gridDim.x - 1) {               // a block of its own: the starts and lengths of all sequences, with tokens or without
+  if (blockIdx.x == 0) {       // a block of its own, the first to run: the starts and lengths of all sequences, with tokens or without
+#pragma unroll 4
     for (int b = threadIdx.x; b < g.B; b += blockDim.x) {
       const int s0 = __ldg(a.q_start + b), s1 = __ldg(a.q_start + b + 1), kv = __ldg(a.kv_len + b);
       if (s0 < 0 || s1 < s0 || s1 > g.n_tokens || kv < 0 || kv > cap) paged_flag(g.status, kBadLength);
@@ -130,7 +131,7 @@ template <bool kF16, int kRows>
 cudaError_t launch(const PagedAppendArgs& a, cudaStream_t st) {
   const int n_rows = (a.q ? a.g.Hq : 0) + 2 * a.g.Hkv;
   const int warps = (n_rows + 4 * kRows - 1) / (4 * kRows);
-  const long long blocks = ((long long)a.g.n_tokens * warps + 7) / 8 + 1;   // (the last looks the starts over)
+  const long long blocks = ((long long)a.g.n_tokens * warps + 7) / 8 + 1;   // (the first looks the starts over)
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   const cudaError_t e = launch_pdl(paged_append_kernel<kF16, kRows>, dim3((unsigned)blocks), dim3(256), 0, st, a, warps);
   if (e == cudaSuccess) count_launch(1);
