@@ -141,10 +141,12 @@ cudaError_t launch(const PagedAppendArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st) {
-  // One row a lane or four: the former while its warps are all resident at once, up to about 27 thousand rows.  Measured, us, one / four,
-  // with 48, 36 and 12 rows a token: 12 thousand rows 3.5 / 4.1, 3.5 / 3.8, 3.7 / 4.0; 24 thousand 4.1 / 4.6, 4.1 / 4.3, 4.1 / 4.3; 28 thousand
-  // 5.0 / 4.7, 4.9 / 4.4, 5.2 / 4.5; 128 thousand 15.7 / 13.2, 15.8 / 14.2, 16.4 / 14.2.  (Two rows a lane: 586 thousand rows 60, four 57.)
-  const bool many = (long long)a.g.n_tokens * ((a.q ? a.g.Hq : 0) + 2 * a.g.Hkv) > 26 * 1024;
+  // One row a lane or four: the former while its warps are all resident at once (40 registers: 48 warps an SM).  Measured, us, one / four,
+  // a token a sequence: 48 rows a token, 500 tokens 4.7 / 4.9, 583 4.7 / 4.7, 666 6.0 / 5.3, 833 7.0 / 6.1; 36 rows, 666 tokens 4.5 / 4.5, 888
+  // 6.0 / 5.1; 10 rows, 2100 tokens 4.5 / 4.4, 2400 5.7 / 4.6, 3200 7.0 / 5.0.  In long appends of 48 rows a token 12 thousand rows 3.5 / 4.1,
+  // 24 thousand 4.1 / 4.6, 28 thousand 5.0 / 4.7, 128 thousand 15.7 / 13.2.  (Two rows a lane: 586 thousand rows 60, four 57.)
+  const int n_rows = (a.q ? a.g.Hq : 0) + 2 * a.g.Hkv;
+  const bool many = (long long)a.g.n_tokens * ((n_rows + 3) / 4) > 48 * kSms;
   if (a.g.f16) return many ? launch<true, 4>(a, st) : launch<true, 1>(a, st);
   return many ? launch<false, 4>(a, st) : launch<false, 1>(a, st);
 }

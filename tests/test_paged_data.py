@@ -347,8 +347,8 @@ def test_a_key_at_minus_infinity_drops_out(cuda_lib, form, dtype):
 
 # ------------------------------------------------------------------------------------------ long appends
 @pytest.mark.parametrize("dtype,Hq,Hkv,T,rot,interleaved,page", [
-    (BF, 32, 8, 553, 128, False, 64),            # just below the number of rows from which a lane takes four
-    (BF, 32, 8, 556, 128, False, 64),            # and just above
+    (BF, 32, 8, 592, 128, False, 64),            # the most tokens of which a lane takes one row
+    (BF, 32, 8, 593, 128, False, 64),            # and the fewest of which it takes four
     (BF, 28, 4, 901, 64, True, 16),
     (FP, 5, 1, 5001, 96, False, 128),            # seven rows a token: most lanes have fewer than four
     (FP, 16, 16, 700, 128, True, 256),
